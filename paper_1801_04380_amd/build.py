@@ -37,7 +37,7 @@ def _stale(target, deps):
 def _compile(src, force):
     obj = os.path.join(OBJ, os.path.basename(src) + ".o")
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    headers += [os.path.join(ROOT, "include", h) for h in ("sn.h", "sn_runtime.h")]
+    headers += [os.path.join(ROOT, "include", h) for h in ("sn.h", "sn_seq.h", "sn_runtime.h")]
     if force or _stale(obj, [src] + headers):
         cmd = ["hipcc"] + FLAGS + ["-c", src, "-o", obj]
         r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -1,0 +1,136 @@
+// What the kernels of the token-sequence layers share: rows of packed sequences, element access at any alignment, sums over lanes.
+#pragma once
+#include "sn_internal.h"
+#include "sn_seq.h"
+
+namespace sn {
+
+template <typename T> __device__ inline float seq_ld(const T *p);
+template <> __device__ inline float seq_ld<float>(const float *p) { return *p; }
+template <> __device__ inline float seq_ld<bf16_t>(const bf16_t *p) { return bf16_to_f32(*p); }
+__device__ inline void seq_st(float *p, float v) { *p = v; }
+__device__ inline void seq_st(bf16_t *p, float v) { *p = f32_to_bf16(v); }
+
+// V neighbouring elements as they lie in memory.  Loaded and stored whole where they are aligned to their size and all there, one by
+// one otherwise; what is not there reads as zero.
+template <typename T, int V> struct alignas(sizeof(T) * V) Pack {
+    T e[V];
+    __device__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = 0;
+    }
+    __device__ void load(const T *p, int n, bool whole)
+    {
+        if (whole && n >= V) {
+            *this = *reinterpret_cast<const Pack *>(p);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = i < n ? p[i] : (T)0;
+    }
+    __device__ void store(T *p, int n, bool whole) const
+    {
+        if (whole && n >= V) {
+            *reinterpret_cast<Pack *>(p) = *this;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = e[i];
+    }
+    __device__ float get(int i) const { return seq_ld<T>(&e[i]); }
+    __device__ void set(int i, float v) { seq_st(&e[i], v); }
+};
+
+// Whether rows that are `ld` elements apart can be accessed V elements at a time.
+inline bool rows_aligned(const void *p, int64_t ld, int esize, int v)
+{
+    return reinterpret_cast<uintptr_t>(p) % (size_t)(esize * v) == 0 && ld % v == 0;
+}
+
+// The rows of packed sequences: off == nullptr: `seqs` sequences of `len` rows.  A row of no sequence has s outside 0 .. seqs - 1.  begin
+// and end stay within 0 .. rows whatever the offsets hold.
+struct SeqRows {
+    const int32_t *off;
+    int seqs, len, rows;
+};
+struct SeqAt {
+    int s, begin, end;  // the sequence of a row, its first row and the one behind its last
+    __device__ bool holds(int row, const SeqRows &r) const { return s >= 0 && s < r.seqs && begin <= row && row < end; }
+};
+__device__ inline SeqAt seq_clamped(const SeqRows &r, int s)
+{
+    SeqAt a;
+    a.s = s;
+    a.begin = s < 0 ? 0 : min(max(r.off[s], 0), r.rows);
+    a.end = s < r.seqs ? min(max(r.off[s + 1], 0), r.rows) : r.rows;
+    return a;
+}
+// The last sequence that begins at or before `row` (s = -1: none does; s = seqs: the row lies behind all of them).
+__device__ inline SeqAt seq_find(const SeqRows &r, int row)
+{
+    if (!r.off) {
+        SeqAt a;
+        a.s = row / r.len;
+        a.begin = a.s * r.len;
+        a.end = a.begin + r.len;
+        return a;
+    }
+    int lo = -1, hi = r.seqs + 1;  // off[lo] <= row < off[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (r.off[mid] <= row) lo = mid; else hi = mid;
+    }
+    return seq_clamped(r, lo);
+}
+// From the place of an earlier row on to that of `row`.
+__device__ inline void seq_forward(const SeqRows &r, SeqAt &a, int row)
+{
+    while (a.s < r.seqs && row >= a.end) {
+        if (r.off) a = seq_clamped(r, a.s + 1);
+        else { ++a.s; a.begin = a.end; a.end += r.len; }
+    }
+}
+
+__device__ inline float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+// a slot index of a step call: row -> slot, or -1 for a row to skip
+__device__ inline int step_slot(const int32_t *slots, int row, int num_slots)
+{
+    const int s = slots ? slots[row] : row;
+    return s >= 0 && s < num_slots ? s : -1;
+}
+
+// ---- launchers (seq_conv1d.hip, seq_headnorm.hip, seq_scan.hip, seq_scan_bwd.hip); arguments checked by seq_api.hip ----
+hipError_t launch_conv1d_fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off,
+                             const void *state_in, void *state_out, hipStream_t st);
+size_t conv1d_scratch_bytes(int64_t rows, int channels, int width);
+hipError_t launch_conv1d_bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias,
+                             const sn_conv1d_shape &s, const int32_t *off, const void *state_in, const void *dstate_out,
+                             void *dstate_in, void *scratch, hipStream_t st);
+hipError_t launch_conv1d_step(const void *x, const void *w, const float *bias, void *y, const void *state, void *state_out,
+                              const int32_t *slots, int num_slots, const sn_conv1d_shape &s, hipStream_t st);
+hipError_t launch_headnorm_fwd(const void *q, const void *k, const float *wq, const float *wk, const int32_t *pos, const float *freq,
+                               void *yq, void *yk, const sn_headnorm_shape &s, hipStream_t st);
+size_t headnorm_scratch_bytes(int64_t rows, int q_heads, int k_heads, int head_dim);
+hipError_t launch_headnorm_bwd(const void *q, const void *k, const float *wq, const float *wk, const int32_t *pos, const float *freq,
+                               const void *dyq, const void *dyk, void *dq, void *dk, float *dwq, float *dwk,
+                               const sn_headnorm_shape &s, void *scratch, hipStream_t st);
+void scan_bwd_bytes(const sn_scan_shape &s, size_t *min_bytes, size_t *preferred_bytes);   // without the states
+void scan_fwd_bytes(const sn_scan_shape &s, size_t *preferred_bytes);
+size_t scan_states_bytes(const sn_scan_shape &s);
+hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
+                           const sn_scan_shape &s, const int32_t *off, const float *h0, float *hT, float *states, void *ws, size_t ws_bytes, hipStream_t st);
+struct ScanGrads {
+    const void *dy;
+    void *du, *ddt, *dB, *dC, *dz;
+    float *dA, *dD, *ddt_bias, *dh0;
+    const float *dhT;
+};
+hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias,
+                           const ScanGrads &g, const sn_scan_shape &s, const int32_t *off, const float *h0, const float *states, void *ws, size_t ws_bytes, hipStream_t st);
+hipError_t launch_scan_step(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
+                            const float *state, float *state_out, const int32_t *slots, int num_slots, const sn_scan_shape &s, hipStream_t st);
+
+}  // namespace sn

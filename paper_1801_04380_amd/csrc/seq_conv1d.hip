@@ -1,0 +1,352 @@
+// The short causal convolution along the tokens (one filter of up to 8 taps per channel, bias and SiLU in the same pass).
+//
+// Two multiplications per tap and a sigmoid per element against two or three tensors read and written: bound by HBM.  A thread owns
+// V neighbouring channels (16 bytes where the rows allow it) and walks down a run of rows with the taps' inputs in registers, so that an
+// input row is loaded once but for the width - 1 rows in front of the run.
+#include "seq.h"
+
+namespace sn {
+namespace {
+
+constexpr int THREADS = 256;
+
+template <typename T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
+
+// The filters and biases of V channels, taps innermost in memory.
+template <typename T, int V, int W> struct Taps {
+    float w[V][W], b[V];
+    __device__ void load(const T *wp, const float *bp, int c, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            b[i] = bp && i < n ? bp[c + i] : 0.f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[i][j] = i < n ? seq_ld<T>(wp + (size_t)(c + i) * W + j) : 0.f;
+        }
+    }
+};
+
+// The input under a tap: row src of x where the sequence that begins at `begin` holds it, a row of the initial state in front of it.
+template <typename T, int V>
+__device__ inline Pack<T, V> tap_input(const T *x, int64_t ld, const T *state, int channels, int W, const SeqAt &at, int src, int c, int n, bool whole)
+{
+    Pack<T, V> v;
+    if (src >= at.begin) v.load(x + (int64_t)src * ld + c, n, whole);
+    else if (state) v.load(state + ((int64_t)at.s * (W - 1) + (W - 1 + src - at.begin)) * channels + c, n, false);
+    else v.zero();
+    return v;
+}
+
+template <typename T, int V, int W>
+__global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, T *__restrict__ y,
+                                                             int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, bool whole_x,
+                                                             bool whole_y, const T *__restrict__ state_in, T *__restrict__ state_out)
+{
+    const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V, n = channels - c;
+    if (n <= 0) return;
+    Taps<T, V, W> taps;
+    taps.load(w, bias, c, n);
+    const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
+    if (r0 < r1) {
+        SeqAt at = seq_find(rows, r0);
+        for (int t = r0; t < r1; ++t) {
+            seq_forward(rows, at, t);
+            if (!at.holds(t, rows)) continue;
+            Pack<T, V> in[W], out;
+#pragma unroll
+            for (int j = 0; j < W; ++j) in[j] = tap_input<T, V>(x, ld_x, state_in, channels, W, at, t - (W - 1) + j, c, n, whole_x);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float p = taps.b[i];
+#pragma unroll
+                for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[j].get(i), p);
+                out.set(i, silu ? p * sigmoid(p) : p);
+            }
+            out.store(y + (int64_t)t * ld_y + c, n, whole_y);
+            if (state_out && t == at.end - 1)
+#pragma unroll
+                for (int j = 1; j < W; ++j) in[j].store(state_out + ((int64_t)at.s * (W - 1) + j - 1) * channels + c, n, false);
+        }
+    }
+    // the states of empty sequences pass through
+    if (state_out && W > 1 && blockIdx.y == 0 && (rows.off || rows.rows == 0))
+        for (int s = 0; s < rows.seqs; ++s) {
+            if (rows.off && rows.off[s] != rows.off[s + 1]) continue;
+            for (int j = 0; j < W - 1; ++j)
+                for (int i = 0; i < min(n, V); ++i) {
+                    const int64_t k = ((int64_t)s * (W - 1) + j) * channels + c + i;
+                    state_out[k] = state_in ? state_in[k] : (T)0;
+                }
+        }
+}
+
+// d y / d p
+__device__ inline float silu_slope(float p)
+{
+    const float s = sigmoid(p);
+    return s * (1.f + p * (1.f - s));
+}
+
+// p of row t, and with it dp.  A row that no sequence holds has none.
+template <typename T, int V, int W>
+__device__ inline void gradient_of_p(const T *x, const T *dy, const T *state, int channels, int silu, int64_t ld_x, int64_t ld_y, const SeqRows &rows, const SeqAt &at,
+                                     int t, int c, int n, bool whole_x, bool whole_y, const Taps<T, V, W> &taps, float (&dp)[V], Pack<T, V> (&in)[W])
+{
+    if (!at.holds(t, rows)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) dp[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) in[j].zero();
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j) in[j] = tap_input<T, V>(x, ld_x, state, channels, W, at, t - (W - 1) + j, c, n, whole_x);
+    Pack<T, V> g;
+    g.load(dy + (int64_t)t * ld_y + c, n, whole_y);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        dp[i] = g.get(i);
+        if (silu) {
+            float p = taps.b[i];
+#pragma unroll
+            for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[j].get(i), p);
+            dp[i] *= silu_slope(p);
+        }
+    }
+}
+
+// part[slice][W + 1][channels]: the slice's sums for dw, then for dbias
+template <typename T, int V, int W>
+__global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, const T *__restrict__ dy,
+                                                             T *__restrict__ dx, float *__restrict__ part, int channels, int silu, int64_t ld_x, int64_t ld_y,
+                                                             int64_t ld_dx, SeqRows rows, int run, bool whole_x, bool whole_y, bool whole_dx,
+                                                             const T *__restrict__ state_in, const T *__restrict__ dstate_out)
+{
+    const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V, n = channels - c;
+    if (n <= 0) return;
+    Taps<T, V, W> taps;
+    taps.load(w, bias, c, n);
+    const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
+    float dw[V][W] = {}, db[V] = {};
+    if (r0 < r1) {
+        SeqAt at = seq_find(rows, r0);
+        for (int t = r0; t < r1; ++t) {
+            seq_forward(rows, at, t);
+            if (!at.holds(t, rows)) continue;
+            float dp[V], g[V] = {};
+            Pack<T, V> in[W], other[W], out;
+#pragma unroll
+            for (int k = W - 1; k >= 0; --k) {
+                if (t + k >= at.end) continue;
+                gradient_of_p<T, V, W>(x, dy, state_in, channels, silu, ld_x, ld_y, rows, at, t + k, c, n, whole_x, whole_y, taps, dp, k == 0 ? in : other);
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[i] = fmaf(taps.w[i][W - 1 - k], dp[i], g[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                db[i] += dp[i];
+#pragma unroll
+                for (int j = 0; j < W; ++j) dw[i][j] = fmaf(dp[i], in[j].get(i), dw[i][j]);
+            }
+            if (dstate_out && t >= at.end - (W - 1))
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i < n) g[i] += seq_ld<T>(dstate_out + ((int64_t)at.s * (W - 1) + t - (at.end - (W - 1))) * channels + c + i);
+#pragma unroll
+            for (int i = 0; i < V; ++i) out.set(i, g[i]);
+            out.store(dx + (int64_t)t * ld_dx + c, n, whole_dx);
+        }
+    }
+    float *to = part + (size_t)blockIdx.y * (W + 1) * channels + c;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < n) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) to[(size_t)j * channels + i] = dw[i][j];
+            to[(size_t)W * channels + i] = db[i];
+        }
+}
+
+// The gradient of the initial states: one thread per sequence and channel.
+template <typename T, int W>
+__global__ void __launch_bounds__(THREADS) conv1d_dstate_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, const T *__restrict__ dy,
+                                                                int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, const T *__restrict__ state_in,
+                                                                const T *__restrict__ dstate_out, T *__restrict__ dstate_in)
+{
+    const int c = blockIdx.y * THREADS + threadIdx.x, s = blockIdx.x;
+    if (c >= channels) return;
+    SeqAt at;
+    if (rows.off) {
+        at = seq_clamped(rows, s);
+    } else {
+        at.s = s; at.begin = s * rows.len; at.end = at.begin + rows.len;
+    }
+    const int len = max(at.end - at.begin, 0);
+    Taps<T, 1, W> taps;
+    taps.load(w, bias, c, 1);
+    float dp[W];  // of the sequence's first rows
+#pragma unroll
+    for (int e = 0; e < W - 1; ++e) {
+        float one[1] = {0.f};
+        Pack<T, 1> in[W];
+        if (e < len) gradient_of_p<T, 1, W>(x, dy, state_in, channels, silu, ld_x, ld_y, rows, at, at.begin + e, c, 1, true, true, taps, one, in);
+        dp[e] = one[0];
+    }
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {   // the state's row i stands W - 1 - i rows in front of the sequence
+        float g = 0.f;
+#pragma unroll
+        for (int e = 0; e <= i; ++e) g = fmaf(taps.w[0][i - e], dp[e], g);   // it is tap i - e of row e
+        const int left = i - len;       // its row in the final state
+        if (dstate_out && left >= 0) g += seq_ld<T>(dstate_out + ((int64_t)s * (W - 1) + left) * channels + c);
+        seq_st(dstate_in + ((int64_t)s * (W - 1) + i) * channels + c, g);
+    }
+}
+
+__global__ void __launch_bounds__(THREADS) conv1d_sum_kernel(const float *__restrict__ part, float *__restrict__ dw, float *__restrict__ dbias, int channels, int width, int slices)
+{
+    const int c = blockIdx.x * THREADS + threadIdx.x, j = blockIdx.y;
+    if (c >= channels) return;
+    float sum = 0.f;
+    for (int s = 0; s < slices; ++s) sum += part[((size_t)s * (width + 1) + j) * channels + c];
+    if (j < width) dw[(size_t)c * width + j] = sum;
+    else if (dbias) dbias[c] = sum;
+}
+
+template <typename T, int V, int W>
+__global__ void __launch_bounds__(THREADS) conv1d_step_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, T *__restrict__ y,
+                                                              const T *state, T *state_out, const int32_t *__restrict__ slots, int num_slots, int channels,
+                                                              int silu, int64_t ld_x, int64_t ld_y, bool whole_x, bool whole_y, bool whole_s)
+{
+    const int c = (blockIdx.y * THREADS + threadIdx.x) * V, n = channels - c, row = blockIdx.x;
+    if (n <= 0) return;
+    const int slot = step_slot(slots, row, num_slots);
+    if (slot < 0) return;
+    Taps<T, V, W> taps;
+    taps.load(w, bias, c, n);
+    Pack<T, V> in[W], out;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) in[j].load(state + ((int64_t)slot * (W - 1) + j) * channels + c, n, whole_s);
+    in[W - 1].load(x + (int64_t)row * ld_x + c, n, whole_x);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        float p = taps.b[i];
+#pragma unroll
+        for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[j].get(i), p);
+        out.set(i, silu ? p * sigmoid(p) : p);
+    }
+    out.store(y + (int64_t)row * ld_y + c, n, whole_y);
+#pragma unroll
+    for (int j = 1; j < W; ++j) in[j].store(state_out + ((int64_t)slot * (W - 1) + j - 1) * channels + c, n, whole_s);
+}
+
+// f(type, width) with both as types
+template <int W> struct WidthIs { static constexpr int value = W; };
+template <typename F> hipError_t by_width(int width, F f)
+{
+    switch (width) {
+    case 1: return f(WidthIs<1>());
+    case 2: return f(WidthIs<2>());
+    case 3: return f(WidthIs<3>());
+    case 4: return f(WidthIs<4>());
+    case 5: return f(WidthIs<5>());
+    case 6: return f(WidthIs<6>());
+    case 7: return f(WidthIs<7>());
+    default: return f(WidthIs<8>());
+    }
+}
+
+SeqRows rows_of(const sn_conv1d_shape &s, const int32_t *off)
+{
+    return {off, s.seqs, (int)(s.rows / s.seqs), (int)s.rows};
+}
+
+int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// Rows of a workgroup's run, a multiple of 16: about 2048 workgroups of `per` channel blocks each, as long as the runs are 16 rows and more.
+int run_of(int64_t rows, int per)
+{
+    const int64_t want = (2048 + per - 1) / per;
+    const int64_t run = ((rows + want - 1) / want + 15) / 16 * 16;
+    return (int)(run < 16 ? 16 : run);
+}
+
+template <typename T> hipError_t fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off, const void *state_in,
+                                     void *state_out, hipStream_t st)
+{
+    constexpr int V = vec_of<T>();
+    return by_width(s.width, [&](auto W) {
+        const int blocks = div_up(s.channels, V * THREADS), run = run_of(s.rows, blocks);
+        conv1d_fwd_kernel<T, V, W.value><<<dim3(blocks, s.rows ? div_up(s.rows, run) : 1), THREADS, 0, st>>>(
+            (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows_of(s, off), run, rows_aligned(x, s.ld_x, sizeof(T), V),
+            rows_aligned(y, s.ld_y, sizeof(T), V), (const T *)state_in, (T *)state_out);
+        return hipGetLastError();
+    });
+}
+
+int bwd_blocks(int channels) { return div_up(channels, 4 * THREADS); }   // the fp32 count, the larger: the scratch does not depend on the type
+
+template <typename T> hipError_t bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
+                                     const int32_t *off, const void *state_in, const void *dstate_out, void *dstate_in, void *scratch, hipStream_t st)
+{
+    constexpr int V = vec_of<T>();
+    return by_width(s.width, [&](auto W) {
+        const int run = run_of(s.rows, bwd_blocks(s.channels)), slices = s.rows ? div_up(s.rows, run) : 1;
+        const SeqRows rows = rows_of(s, off);
+        conv1d_bwd_kernel<T, V, W.value><<<dim3(div_up(s.channels, V * THREADS), slices), THREADS, 0, st>>>(
+            (const T *)x, (const T *)w, bias, (const T *)dy, (T *)dx, (float *)scratch, s.channels, s.silu, s.ld_x, s.ld_y, s.ld_dx, rows, run,
+            rows_aligned(x, s.ld_x, sizeof(T), V), rows_aligned(dy, s.ld_y, sizeof(T), V), rows_aligned(dx, s.ld_dx, sizeof(T), V), (const T *)state_in,
+            (const T *)dstate_out);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        conv1d_sum_kernel<<<dim3(div_up(s.channels, THREADS), s.width + 1), THREADS, 0, st>>>((const float *)scratch, dw, dbias, s.channels, s.width, slices);
+        e = hipGetLastError();
+        if (e != hipSuccess || !dstate_in || s.width == 1) return e;
+        conv1d_dstate_kernel<T, W.value><<<dim3(s.seqs, div_up(s.channels, THREADS)), THREADS, 0, st>>>(
+            (const T *)x, (const T *)w, bias, (const T *)dy, s.channels, s.silu, s.ld_x, s.ld_y, rows, (const T *)state_in, (const T *)dstate_out, (T *)dstate_in);
+        return hipGetLastError();
+    });
+}
+
+template <typename T> hipError_t step(const void *x, const void *w, const float *bias, void *y, const void *state, void *state_out, const int32_t *slots, int num_slots,
+                                      const sn_conv1d_shape &s, hipStream_t st)
+{
+    constexpr int V = vec_of<T>();
+    return by_width(s.width, [&](auto W) {
+        const bool whole_s = rows_aligned(state, s.channels, sizeof(T), V) && rows_aligned(state_out, s.channels, sizeof(T), V);
+        conv1d_step_kernel<T, V, W.value><<<dim3((int)s.rows, div_up(s.channels, V * THREADS)), THREADS, 0, st>>>(
+            (const T *)x, (const T *)w, bias, (T *)y, (const T *)state, (T *)state_out, slots, num_slots, s.channels, s.silu, s.ld_x, s.ld_y,
+            rows_aligned(x, s.ld_x, sizeof(T), V), rows_aligned(y, s.ld_y, sizeof(T), V), whole_s);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+hipError_t launch_conv1d_fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off, const void *state_in,
+                             void *state_out, hipStream_t st)
+{
+    return s.dtype == SN_BF16 ? fwd<bf16_t>(x, w, bias, y, s, off, state_in, state_out, st) : fwd<float>(x, w, bias, y, s, off, state_in, state_out, st);
+}
+
+size_t conv1d_scratch_bytes(int64_t rows, int channels, int width)
+{
+    const int slices = rows ? div_up(rows, run_of(rows, bwd_blocks(channels))) : 1;
+    return align_up((size_t)slices * (width + 1) * channels * 4, 256);
+}
+
+hipError_t launch_conv1d_bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
+                             const int32_t *off, const void *state_in, const void *dstate_out, void *dstate_in, void *scratch, hipStream_t st)
+{
+    return s.dtype == SN_BF16 ? bwd<bf16_t>(x, w, bias, dy, dx, dw, dbias, s, off, state_in, dstate_out, dstate_in, scratch, st)
+                              : bwd<float>(x, w, bias, dy, dx, dw, dbias, s, off, state_in, dstate_out, dstate_in, scratch, st);
+}
+
+hipError_t launch_conv1d_step(const void *x, const void *w, const float *bias, void *y, const void *state, void *state_out, const int32_t *slots, int num_slots,
+                              const sn_conv1d_shape &s, hipStream_t st)
+{
+    return s.dtype == SN_BF16 ? step<bf16_t>(x, w, bias, y, state, state_out, slots, num_slots, s, st)
+                              : step<float>(x, w, bias, y, state, state_out, slots, num_slots, s, st);
+}
+
+}  // namespace sn

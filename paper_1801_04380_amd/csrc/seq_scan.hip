@@ -1,0 +1,347 @@
+// The selective state space scan, forward and for single tokens.
+//
+//   h[d,n] = exp(delta A[d,n]) h[d,n] + delta u B[n],   y = sum_n C[n] h[d,n] + D u,   times z sigmoid(z)
+//
+// Per row, channel and state: a product, an exponential (a quarter of the rate), and three products and sums: eight issue slots, against
+// four tensors of rows x channels read and written.  With 16 states that is more time on the vector units than in HBM.
+// Where channels and sequences alone do not fill the chip the tokens are cut into chunks: a first pass takes every chunk's
+// final state from a zero one and its sum of delta (the product of its decays is exp(A * sum)), scan_carry_kernel joins them, and the
+// second pass starts each chunk from its state.
+#include "seq_scan.h"
+
+namespace sn {
+namespace {
+
+constexpr int THREADS = 256;
+
+// MODE 0: y (and, if asked for, the states of tiles and the final states); 1: the chunk's final state from zero and the sum of delta;
+// 2: the states of tiles alone.
+template <typename T, int NL, int MODE>
+__global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
+{
+    using G = ScanGeo<NL>;
+    constexpr int CB = G::CB, NP = G::NP, VE = G::VE;
+    constexpr bool OUT = MODE == 0, LOCAL = MODE == 1;
+    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_y[OUT ? TS : 1][OUT ? CB : 1];
+    __shared__ alignas(16) float s_B[TS * NP];
+    __shared__ alignas(16) float s_C[OUT ? TS * NP : 4];
+
+    const int chunk = blockIdx.x, span = chunk / a.parts, part = chunk % a.parts;
+    if (LOCAL && part == a.parts - 1) return;   // nothing comes after it
+    const int group = blockIdx.y / a.blocks_per_group, inside = blockIdx.y % a.blocks_per_group * CB;
+    const int c0 = group * a.per_group + inside, nch = min(CB, a.per_group - inside);
+    const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
+    const ScanLane<NL> lane(a, c0, nch);
+    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = (threadIdx.x & 63) / G::CW;
+
+    float bias[VE], skip[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        bias[i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
+        skip[i] = OUT && a.D && i < nco ? a.D[c0 + co + i] : 0.f;
+    }
+    float h[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
+    bool crossed = false;
+    if (!LOCAL && part > 0) lane.load(a.carry, chunk, a, h);
+
+    if (r0 < r1) {
+        SeqAt at = seq_find(a.rows, r0);
+        TileAt m = tile_at(a.rows, at, r0, r1, true);
+        Staged<T, NL> u, dt, z;
+        StagedBC<T, NL> B, C;
+        const auto fetch = [&](int t0) {
+            const bool in = m.valid >> row & 1;
+            const int64_t t = t0 + row;
+            const int n = in ? nco : 0;
+            u.load(a.u, t * a.ld_u + c0 + co, n, a.whole_u);
+            dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
+            if (OUT && a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
+            B.load(a.B, a.ld_b, t0, (int64_t)group * a.N, a.N, m.valid);
+            if (OUT) C.load(a.C, a.ld_c, t0, (int64_t)group * a.N, a.N, m.valid);
+        };
+        fetch(r0);
+        for (int t0 = r0; t0 < r1; t0 += TS) {
+            const bool in = m.valid >> row & 1;
+            float uu[VE], gate[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                const float raw = dt.get(i) + bias[i], delta = in && i < nco ? (a.softplus ? softplus(raw) : raw) : 0.f;
+                uu[i] = u.get(i);
+                s_delta[row][co + i] = delta;
+                s_x[row][co + i] = delta * uu[i];
+                gate[i] = 1.f;
+                if (OUT && a.z) gate[i] = z.get(i) * sigmoid(z.get(i));
+            }
+            B.put(s_B);
+            if (OUT) C.put(s_C);
+            const TileAt now = m;
+            __syncthreads();
+            if (t0 + TS < r1) {
+                m = tile_at(a.rows, at, t0 + TS, r1, true);
+                fetch(t0 + TS);
+            }
+            if (!LOCAL && a.states) lane.store(a.states, (int64_t)span * a.tiles_per_span + (t0 - span * a.span_rows) / TS, a, h);
+
+            float acc[NL];
+            const auto step = [&](int t) {
+                const float delta = s_delta[t][lane.c], x = s_x[t][lane.c];
+                const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
+                float4 c = {};
+                if (OUT) c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    h[i] = fmaf(exp2_fast(delta * lane.A2[i]), h[i], x * bb[i]);
+                    sum = fmaf(h[i], cc[i], sum);
+                }
+                acc[t % NL] = sum;
+                if (LOCAL) sum_delta += delta;
+            };
+            const auto reset = [&](int t) {
+                crossed = true;
+                sum_delta = 0.f;
+                if (a.h0) lane.load(a.h0, now.of(t), a, h);
+                else h[0] = h[1] = h[2] = h[3] = 0.f;
+            };
+            const auto flush = [&](int t) {   // rows t + 1 - NL .. t are done
+                if (OUT) s_y[t / NL * NL + nl][lane.c] = scatter_sum<32, G::CW>(acc);
+            };
+            if (!(now.start & ~1u) && !(now.end & (now.end - 1))) {
+                // one sequence; rows behind its end leave h as it is
+                if (now.start) reset(0);
+#pragma unroll
+                for (int t = 0; t < TS; ++t) {
+                    step(t);
+                    if (t % NL == NL - 1) flush(t);
+                }
+                if (OUT && a.hT && now.end) lane.store(a.hT, now.of(__builtin_ctz(now.end)), a, h);
+            } else {
+                for (int tb = 0; tb < TS; tb += NL) {
+#pragma unroll
+                    for (int i = 0; i < NL; ++i) {
+                        const int t = tb + i;
+                        if (now.start >> t & 1) reset(t);
+                        step(t);
+                        if (OUT && a.hT && (now.end >> t & 1)) lane.store(a.hT, now.of(t), a, h);
+                    }
+                    flush(tb + NL - 1);
+                }
+            }
+            __syncthreads();
+            if (OUT && in) {
+                Staged<T, NL> y;
+#pragma unroll
+                for (int i = 0; i < VE; ++i) y.set(i, fmaf(skip[i], uu[i], s_y[row][co + i]) * gate[i]);
+                y.store(a.y, (int64_t)(t0 + row) * a.ld_y + c0 + co, nco, a.whole_y);
+            }
+        }
+    }
+    if (LOCAL) {
+        lane.store(a.carry, chunk, a, h);
+        if (lane.n0 == 0 && lane.there) a.sum_delta[(int64_t)chunk * a.channels + lane.channel] = sum_delta;
+        if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
+    }
+    if (OUT && a.hT && chunk == 0 && (a.rows.off || a.rows.rows == 0))
+        for (int s = 0; s < a.rows.seqs; ++s) {   // the states of empty sequences pass through
+            if (a.rows.off && a.rows.off[s] != a.rows.off[s + 1]) continue;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.h0) lane.load(a.h0, s, a, v);
+            lane.store(a.hT, s, a, v);
+        }
+}
+
+// The state that each chunk starts from, in place of the one that it ends with from zero.  Reverse: the gradient of the state that
+// reaches a chunk from the one behind it.
+__global__ void __launch_bounds__(THREADS) scan_carry_kernel(ScanArgs a, int reverse)
+{
+    const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.N;
+    if (i >= each) return;
+    const int channel = (int)(i / a.N);
+    const float A2 = a.A[i] * 1.44269504088896340736f;
+    float v = 0.f;
+    for (int k = 0; k < a.parts; ++k) {
+        const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - k : k);
+        float local = 0.f;
+        bool through = false;
+        float sum = 0.f;
+        if (k < a.parts - 1) {
+            local = a.carry[chunk * each + i];
+            through = a.through[chunk];
+            sum = a.sum_delta[chunk * a.channels + channel];
+        }
+        a.carry[chunk * each + i] = v;
+        v = through ? fmaf(exp2_fast(A2 * sum), v, local) : local;
+    }
+}
+
+// One token: a thread holds four states of a channel, NL neighbouring threads a channel.
+template <typename T, int NL>
+__global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const float *state, float *state_out, const int32_t *slots, int num_slots)
+{
+    const int slot = step_slot(slots, blockIdx.x, num_slots);
+    if (slot < 0) return;
+    const int64_t t = blockIdx.x;
+    const int k = blockIdx.y * THREADS + threadIdx.x, c = k / NL, n0 = k % NL * 4;
+    if (c >= a.channels) return;
+    const int group = c / a.per_group;
+    const float u = seq_ld<T>((const T *)a.u + t * a.ld_u + c);
+    float raw = seq_ld<T>((const T *)a.dt + t * a.ld_dt + c);
+    if (a.bias) raw += a.bias[c];
+    const float delta = a.softplus ? softplus(raw) : raw;
+    const T *B = (const T *)a.B + t * a.ld_b + (int64_t)group * a.N + n0, *C = (const T *)a.C + t * a.ld_c + (int64_t)group * a.N + n0;
+    const float *from = state + ((int64_t)slot * a.channels + c) * a.N + n0, *A = a.A + (int64_t)c * a.N + n0;
+    float *to = state_out + ((int64_t)slot * a.channels + c) * a.N + n0;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (n0 + i >= a.N) continue;
+        const float h = fmaf(expf(delta * A[i]), from[i], delta * u * seq_ld<T>(B + i));
+        sum = fmaf(h, seq_ld<T>(C + i), sum);
+        to[i] = h;
+    }
+#pragma unroll
+    for (int m = NL / 2; m >= 1; m /= 2) sum += __shfl_xor(sum, m, 64);
+    if (n0) return;
+    float y = a.D ? fmaf(a.D[c], u, sum) : sum;
+    if (a.z) {
+        const float z = seq_ld<T>((const T *)a.z + t * a.ld_z + c);
+        y *= z * sigmoid(z);
+    }
+    seq_st((T *)a.y + t * a.ld_y + c, y);
+}
+
+template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st)
+{
+    return by_lanes(p.NL, [&](auto NL) {
+        const dim3 grid(p.chunks, p.blocks);
+        if (s.dtype == SN_BF16) scan_fwd_kernel<bf16_t, NL.value, MODE><<<grid, THREADS, 0, st>>>(a);
+        else scan_fwd_kernel<float, NL.value, MODE><<<grid, THREADS, 0, st>>>(a);
+        return hipGetLastError();
+    });
+}
+
+int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+}  // namespace
+
+ScanPlan scan_plan(const sn_scan_shape &s, int parts)
+{
+    ScanPlan p;
+    p.NL = s.states <= 8 ? 2 : s.states <= 16 ? 4 : s.states <= 32 ? 8 : 16;
+    p.CB = 256 / p.NL;
+    p.blocks_per_group = div_up(s.channels / s.groups, p.CB);
+    p.blocks = p.blocks_per_group * s.groups;
+    p.spans = s.ragged || s.rows == 0 ? 1 : s.seqs;
+    p.span_rows = (int)(s.rows / p.spans);
+    p.tiles_per_span = div_up(p.span_rows, TS);
+    if (parts < 1) parts = 1;
+    const int tiles = p.tiles_per_span ? div_up(p.tiles_per_span, parts) : 1;
+    p.chunk_rows = tiles * TS;
+    p.parts = p.tiles_per_span ? div_up(p.tiles_per_span, tiles) : 1;
+    p.chunks = p.spans * p.parts;
+    return p;
+}
+
+// Into how many chunks a span is cut when there is workspace for it.
+int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
+{
+    const ScanPlan p = scan_plan(s, 1);
+    const int64_t have = (int64_t)p.blocks * p.spans, want = 512;
+    if (have >= want / 2) return 1;
+    int64_t parts = (want + have - 1) / have;
+    const int64_t most = p.tiles_per_span / 4;   // chunks of 64 rows at least
+    if (parts > most) parts = most;
+    return parts < 1 ? 1 : (int)parts;
+}
+
+size_t scan_carry_bytes(const sn_scan_shape &s, const ScanPlan &p)
+{
+    if (p.parts == 1) return 0;
+    return align_up((size_t)p.chunks * s.channels * s.states * 4, 256) + align_up((size_t)p.chunks * s.channels * 4, 256) + align_up((size_t)p.chunks * 4, 256);
+}
+
+ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off)
+{
+    ScanArgs a = {};
+    a.ld_u = s.ld_u; a.ld_dt = s.ld_dt; a.ld_b = s.ld_b; a.ld_c = s.ld_c; a.ld_z = s.ld_z; a.ld_y = s.ld_y;
+    a.ld_du = s.ld_du; a.ld_ddt = s.ld_ddt; a.ld_db = s.ld_db; a.ld_dc = s.ld_dc; a.ld_dz = s.ld_dz;
+    a.rows = {off, s.seqs, (int)(s.rows / s.seqs), (int)s.rows};
+    a.channels = s.channels; a.N = s.states; a.per_group = s.channels / s.groups; a.blocks_per_group = p.blocks_per_group; a.softplus = s.softplus;
+    a.span_rows = p.span_rows; a.chunk_rows = p.chunk_rows; a.parts = p.parts; a.spans = p.spans; a.tiles_per_span = p.tiles_per_span;
+    return a;
+}
+
+// Whether the rows of a tensor can be staged in whole pieces: its address, its stride and every block's first channel.
+int scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan)
+{
+    const int e = s.dtype == SN_BF16 ? 2 : 4, ve = plan.CB / 16, piece = ve * e > 16 ? 16 / e : ve;
+    return rows_aligned(p, ld, e, piece) && (s.groups == 1 || s.channels / s.groups % piece == 0);
+}
+
+void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws)
+{
+    char *at = (char *)ws;
+    a.carry = (float *)at;
+    at += align_up((size_t)p.chunks * s.channels * s.states * 4, 256);
+    a.sum_delta = (float *)at;
+    at += align_up((size_t)p.chunks * s.channels * 4, 256);
+    a.through = (int *)at;
+}
+
+size_t scan_states_bytes(const sn_scan_shape &s)
+{
+    const ScanPlan p = scan_plan(s, 1);
+    return align_up((size_t)p.spans * p.tiles_per_span * s.channels * s.states * 4, 256);
+}
+
+void scan_fwd_bytes(const sn_scan_shape &s, size_t *preferred_bytes) { *preferred_bytes = scan_carry_bytes(s, scan_plan(s, scan_parts_wanted(s, false))); }
+
+hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st)
+{
+    scan_carry_kernel<<<dim3(div_up((int64_t)a.channels * a.N, THREADS), p.spans), THREADS, 0, st>>>(a, reverse);
+    return hipGetLastError();
+}
+
+template <int MODE> static hipError_t fwd_in_chunks(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st)
+{
+    if (p.parts > 1) {
+        ScanArgs local = a;
+        local.states = nullptr;
+        hipError_t e = launch_fwd<1>(local, s, p, st);
+        if (e == hipSuccess) e = launch_scan_carry(a, p, false, st);
+        if (e != hipSuccess) return e;
+    }
+    return launch_fwd<MODE>(a, s, p, st);
+}
+
+hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st) { return fwd_in_chunks<2>(a, s, p, st); }
+
+hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
+                           const sn_scan_shape &s, const int32_t *off, const float *h0, float *hT, float *states, void *ws, size_t ws_bytes, hipStream_t st)
+{
+    ScanPlan p = scan_plan(s, scan_parts_wanted(s, false));
+    while (p.parts > 1 && scan_carry_bytes(s, p) > ws_bytes) p = scan_plan(s, p.parts - 1);
+    ScanArgs a = scan_args(s, p, off);
+    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.bias = bias; a.y = y; a.h0 = h0; a.hT = hT; a.states = states;
+    a.whole_u = scan_whole_rows(u, s.ld_u, s, p); a.whole_dt = scan_whole_rows(dt, s.ld_dt, s, p); a.whole_y = scan_whole_rows(y, s.ld_y, s, p);
+    a.whole_z = z && scan_whole_rows(z, s.ld_z, s, p);
+    if (p.parts > 1) scan_set_carry(a, s, p, ws);
+    return fwd_in_chunks<0>(a, s, p, st);
+}
+
+hipError_t launch_scan_step(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
+                            const float *state, float *state_out, const int32_t *slots, int num_slots, const sn_scan_shape &s, hipStream_t st)
+{
+    const ScanPlan p = scan_plan(s, 1);
+    ScanArgs a = scan_args(s, p, nullptr);
+    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.bias = bias; a.y = y;
+    const dim3 grid((int)s.rows, div_up((int64_t)s.channels * p.NL, THREADS));
+    return by_lanes(p.NL, [&](auto NL) {
+        if (s.dtype == SN_BF16) scan_step_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+        else scan_step_kernel<float, NL.value><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace sn

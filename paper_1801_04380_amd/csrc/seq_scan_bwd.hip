@@ -1,0 +1,407 @@
+// The gradients of the selective state space scan.
+//
+// With gy = dy z sigmoid(z) the gradient of the states runs backwards along the tokens,
+//   g[t] = gy[t] C[t] + exp(delta[t+1] A) g[t+1],
+// and everything else is made of it and of the states h:
+//   du = gy D + delta sum_n g B        ddelta = u sum_n g B + sum_n A q,  q = g exp(delta A) h[t-1]        dA = sum_t delta q
+//   dB = sum_d g delta u               dC = sum_d gy h
+// A tile's states are computed again from the one kept before it (16 rows of states and decays in registers, four states a lane),
+// then the tile is walked backwards.  Three sums over a channel's states and two over a group's channels per row come on top of the
+// products: scatter_sum shares an exchange among as many values as it has lanes, 8 values a row and lane for dB and dC.  The sums of a
+// workgroup's channels go to the workspace and are joined by scan_join_kernel, in a fixed order.  Bound by the vector units.
+// Cut into chunks like the forward pass where channels and sequences do not fill the chip: scan_bwd_local_kernel takes what a chunk hands to
+// the one before it, scan_carry_kernel joins.
+#include "seq_scan.h"
+
+namespace sn {
+namespace {
+
+constexpr int THREADS = 256;
+
+// What of the gradient of the states a chunk hands on to the one before it, starting from zero, and its sum of delta.
+template <typename T, int NL>
+__global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
+{
+    using G = ScanGeo<NL>;
+    constexpr int CB = G::CB, NP = G::NP, VE = G::VE;
+    __shared__ float s_delta[TS][CB], s_g[TS][CB];
+    __shared__ alignas(16) float s_C[TS * NP];
+    const int chunk = blockIdx.x, span = chunk / a.parts, part = chunk % a.parts;
+    if (part == 0) return;   // nothing comes before it
+    const int group = blockIdx.y / a.blocks_per_group, inside = blockIdx.y % a.blocks_per_group * CB;
+    const int c0 = group * a.per_group + inside, nch = min(CB, a.per_group - inside);
+    const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
+    const ScanLane<NL> lane(a, c0, nch);
+    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co;
+    float bias[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) bias[i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
+    float g[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
+    bool crossed = false;
+    SeqAt at = seq_find(a.rows, r1 - 1);
+    const int last = r0 + (r1 - 1 - r0) / TS * TS;
+    for (int t0 = last; t0 >= r0; t0 -= TS) {
+        const TileAt m = tile_at(a.rows, at, t0, r1, false);
+        const bool in = m.valid >> row & 1;
+        const int n = in ? nco : 0;
+        const int64_t t = t0 + row;
+        Staged<T, NL> dt, z, dy;
+        StagedBC<T, NL> C;
+        dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
+        dy.load(a.dy, t * a.ld_y + c0 + co, n, a.whole_y);
+        if (a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
+        C.load(a.C, a.ld_c, t0, (int64_t)group * a.N, a.N, m.valid);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+            const float raw = dt.get(i) + bias[i];
+            s_delta[row][co + i] = in && i < nco ? (a.softplus ? softplus(raw) : raw) : 0.f;
+            s_g[row][co + i] = dy.get(i) * (a.z ? z.get(i) * sigmoid(z.get(i)) : 1.f);
+        }
+        C.put(s_C);
+        __syncthreads();
+#pragma unroll
+        for (int k = TS - 1; k >= 0; --k) {
+            if (m.end >> k & 1) {
+                crossed = true;
+                sum_delta = 0.f;
+                if (a.dhT) lane.load(a.dhT, m.of(k), a, g);
+                else g[0] = g[1] = g[2] = g[3] = 0.f;
+            }
+            const float delta = s_delta[k][lane.c], gy = s_g[k][lane.c];
+            const float4 c = *reinterpret_cast<const float4 *>(&s_C[k * NP + lane.n0]);
+            const float cc[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] = exp2_fast(delta * lane.A2[i]) * fmaf(gy, cc[i], g[i]);
+            sum_delta += delta;
+        }
+    }
+    lane.store(a.carry, chunk, a, g);
+    if (lane.n0 == 0 && lane.there) a.sum_delta[(int64_t)chunk * a.channels + lane.channel] = sum_delta;
+    if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
+}
+
+template <typename T, int NL>
+__global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanArgs a)
+{
+    using G = ScanGeo<NL>;
+    constexpr int CB = G::CB, NP = G::NP, VE = G::VE, CW = G::CW;
+    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_g[TS][CB], s_y[TS][CB];
+    __shared__ alignas(16) float s_B[TS * NP], s_C[TS * NP];
+    __shared__ float s_bc[4][TS][2 * NP];
+
+    const int chunk = blockIdx.x, span = chunk / a.parts, part = chunk % a.parts;
+    const int group = blockIdx.y / a.blocks_per_group, inside = blockIdx.y % a.blocks_per_group * CB;
+    const int c0 = group * a.per_group + inside, nch = min(CB, a.per_group - inside);
+    const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
+    const ScanLane<NL> lane(a, c0, nch);
+    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = (threadIdx.x & 63) / CW, wave = threadIdx.x / 64;
+    float bias[VE], skip[VE], dD[VE], dbias[VE], A[4], dA[4];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        bias[i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
+        skip[i] = a.D && i < nco ? a.D[c0 + co + i] : 0.f;
+        dD[i] = dbias[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        A[i] = lane.there && lane.n0 + i < a.N ? a.A[(int64_t)lane.channel * a.N + lane.n0 + i] : 0.f;
+        dA[i] = 0.f;
+    }
+    float g[4] = {0.f, 0.f, 0.f, 0.f};
+    if (part < a.parts - 1) lane.load(a.carry, chunk, a, g);
+
+    if (r0 < r1) {
+        SeqAt at = seq_find(a.rows, r1 - 1);
+        const int last = r0 + (r1 - 1 - r0) / TS * TS;
+        TileAt m = tile_at(a.rows, at, last, r1, false);
+        Staged<T, NL> u, dt, z, dy;
+        StagedBC<T, NL> B, C;
+        const auto fetch = [&](int t0) {
+            const int64_t t = t0 + row;
+            const int n = m.valid >> row & 1 ? nco : 0;
+            u.load(a.u, t * a.ld_u + c0 + co, n, a.whole_u);
+            dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
+            dy.load(a.dy, t * a.ld_y + c0 + co, n, a.whole_y);
+            if (a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
+            B.load(a.B, a.ld_b, t0, (int64_t)group * a.N, a.N, m.valid);
+            C.load(a.C, a.ld_c, t0, (int64_t)group * a.N, a.N, m.valid);
+        };
+        fetch(last);
+        for (int t0 = last; t0 >= r0; t0 -= TS) {
+            const bool in = m.valid >> row & 1;
+            float uu[VE], raw[VE], delta[VE], gy[VE], dyv[VE], zz[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                raw[i] = dt.get(i) + bias[i];
+                delta[i] = in && i < nco ? (a.softplus ? softplus(raw[i]) : raw[i]) : 0.f;
+                uu[i] = u.get(i);
+                dyv[i] = dy.get(i);
+                zz[i] = a.z ? z.get(i) : 0.f;
+                gy[i] = a.z ? dyv[i] * zz[i] * sigmoid(zz[i]) : dyv[i];
+                s_delta[row][co + i] = delta[i];
+                s_x[row][co + i] = delta[i] * uu[i];
+                s_g[row][co + i] = gy[i];
+            }
+            B.put(s_B);
+            C.put(s_C);
+            const TileAt now = m;
+            __syncthreads();
+            if (t0 - TS >= r0) {
+                m = tile_at(a.rows, at, t0 - TS, r1, false);
+                fetch(t0 - TS);
+            }
+
+            // the states of the tile, forwards
+            float hs[TS][4], decay[TS][4], first[4], acc[NL];
+            const bool one = !(now.start & ~1u) && !(now.end & (now.end - 1));
+            if (now.start & 1) {
+                if (a.h0) lane.load(a.h0, now.of(0), a, first);
+                else first[0] = first[1] = first[2] = first[3] = 0.f;
+            } else {
+                lane.load(a.states, (int64_t)span * a.tiles_per_span + (t0 - span * a.span_rows) / TS, a, first);
+            }
+#pragma unroll
+            for (int t = 0; t < TS; ++t) {
+                const float d = s_delta[t][lane.c], x = s_x[t][lane.c];
+                const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                float past[4], sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) past[i] = t ? hs[t ? t - 1 : 0][i] : first[i];
+                if (!one && t && (now.start >> t & 1)) {
+                    if (a.h0) lane.load(a.h0, now.of(t), a, past);
+                    else past[0] = past[1] = past[2] = past[3] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    decay[t][i] = exp2_fast(d * lane.A2[i]);
+                    hs[t][i] = fmaf(decay[t][i], past[i], x * bb[i]);
+                    sum = fmaf(hs[t][i], cc[i], sum);
+                }
+                acc[t % NL] = sum;
+                if (t % NL == NL - 1) {
+                    const float y = scatter_sum<32, CW>(acc);
+                    if (a.z) s_y[t / NL * NL + nl][lane.c] = y;
+                }
+            }
+            // and its gradients, backwards
+            float gb[NL], qa[NL], bc[CW < 8 ? 8 : CW];
+#pragma unroll
+            for (int t = TS - 1; t >= 0; --t) {
+                if (now.end >> t & 1) {
+                    if (a.dhT) lane.load(a.dhT, now.of(t), a, g);
+                    else g[0] = g[1] = g[2] = g[3] = 0.f;
+                }
+                const float d = s_delta[t][lane.c], x = s_x[t][lane.c], gyt = s_g[t][lane.c];
+                const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                float past[4], sum_b = 0.f, sum_a = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) past[i] = t ? hs[t ? t - 1 : 0][i] : first[i];
+                if (!one && t && (now.start >> t & 1)) {
+                    if (a.h0) lane.load(a.h0, now.of(t), a, past);
+                    else past[0] = past[1] = past[2] = past[3] = 0.f;
+                }
+                constexpr int TB = CW < 8 ? 1 : CW / 8;   // rows whose 8 values share the exchanges over channels
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float gi = fmaf(gyt, cc[i], g[i]);
+                    bc[t % TB * 8 + i] = gi * x;
+                    bc[t % TB * 8 + 4 + i] = gyt * hs[t][i];
+                    sum_b = fmaf(gi, bb[i], sum_b);
+                    g[i] = decay[t][i] * gi;
+                    const float q = g[i] * past[i];
+                    sum_a = fmaf(q, A[i], sum_a);
+                    dA[i] = fmaf(q, d, dA[i]);
+                }
+                if (a.dh0 && (now.start >> t & 1)) lane.store(a.dh0, now.of(t), a, g);
+                gb[t % NL] = sum_b;
+                qa[t % NL] = sum_a;
+                if (t % NL == 0) {   // rows t .. t + NL - 1 are done: their places take the sums
+                    const float vb = scatter_sum<32, CW>(gb), va = scatter_sum<32, CW>(qa);
+                    s_x[t + nl][lane.c] = vb;
+                    s_delta[t + nl][lane.c] = va;
+                }
+                if (t % TB == 0) {
+                    const int low = threadIdx.x & (CW - 1);
+                    if constexpr (CW >= 8) {
+                        const float v = scatter_sum<CW / 2, 1>(bc);
+                        s_bc[wave][t + low / 8][(low / 4 & 1) * NP + lane.n0 + low % 4] = v;
+                    } else {
+                        float lo[4] = {bc[0], bc[1], bc[2], bc[3]}, hi[4] = {bc[4], bc[5], bc[6], bc[7]};
+                        s_bc[wave][t][lane.n0 + low] = scatter_sum<2, 1>(lo);
+                        s_bc[wave][t][NP + lane.n0 + low] = scatter_sum<2, 1>(hi);
+                    }
+                }
+            }
+            __syncthreads();
+            if (in) {
+                const int64_t t = t0 + row;
+                Staged<T, NL> o;
+                float dd[VE];
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    const float vb = s_x[row][co + i], va = s_delta[row][co + i];
+                    o.set(i, fmaf(gy[i], skip[i], delta[i] * vb));
+                    dd[i] = fmaf(uu[i], vb, va);
+                    if (a.softplus) dd[i] *= sigmoid(raw[i]);
+                    if (i < nco) {
+                        dbias[i] += dd[i];
+                        dD[i] = fmaf(gy[i], uu[i], dD[i]);
+                    }
+                }
+                o.store(a.du, t * a.ld_du + c0 + co, nco, a.whole_du);
+#pragma unroll
+                for (int i = 0; i < VE; ++i) o.set(i, dd[i]);
+                o.store(a.ddt, t * a.ld_ddt + c0 + co, nco, a.whole_ddt);
+                if (a.z) {
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) {
+                        const float s = sigmoid(zz[i]);
+                        o.set(i, dyv[i] * fmaf(skip[i], uu[i], s_y[row][co + i]) * s * (1.f + zz[i] * (1.f - s)));
+                    }
+                    o.store(a.dz, t * a.ld_dz + c0 + co, nco, a.whole_dz);
+                }
+            }
+            for (int k = threadIdx.x; k < TS * 2 * NP; k += THREADS) {
+                const int r = k / (2 * NP), n = k % (2 * NP);
+                if (now.valid >> r & 1)
+                    a.part_bc[((int64_t)blockIdx.y * a.rows.rows + t0 + r) * (2 * NP) + n] = s_bc[0][r][n] + s_bc[1][r][n] + s_bc[2][r][n] + s_bc[3][r][n];
+            }
+            __syncthreads();
+        }
+    }
+    lane.store(a.part_a, chunk, a, dA);
+    // dD and the bias's gradient: over the 16 threads that stage a channel
+    for (int what = 0; what < 2; ++what) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VE; ++i) s_x[row][co + i] = what ? dbias[i] : dD[i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < nch; c += THREADS) {
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < TS; ++r) sum += s_x[r][c];
+            (what ? a.part_bias : a.part_d)[(int64_t)chunk * a.channels + c0 + c] = sum;
+        }
+    }
+    if (a.dh0 && chunk == 0 && (a.rows.off || a.rows.rows == 0))
+        for (int s = 0; s < a.rows.seqs; ++s) {   // through empty sequences
+            if (a.rows.off && a.rows.off[s] != a.rows.off[s + 1]) continue;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.dhT) lane.load(a.dhT, s, a, v);
+            lane.store(a.dh0, s, a, v);
+        }
+}
+
+// dB and dC from the sums of the channel blocks: one thread per row, group, tensor and state.
+template <typename T>
+__global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int groups, int NP)
+{
+    const int64_t k = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+    const int n = (int)(k % NP), which = (int)(k / NP % 2), group = (int)(k / (2 * NP) % groups);
+    const int64_t row = k / (2 * NP) / groups;
+    if (row >= a.rows.rows || n >= a.N) return;
+    if (a.rows.off && !seq_find(a.rows, (int)row).holds((int)row, a.rows)) return;
+    float sum = 0.f;
+    for (int b = 0; b < a.blocks_per_group; ++b)
+        sum += a.part_bc[(((int64_t)group * a.blocks_per_group + b) * a.rows.rows + row) * (2 * NP) + which * NP + n];
+    T *to = which ? (T *)a.dC + row * a.ld_dc : (T *)a.dB + row * a.ld_db;
+    seq_st(to + (int64_t)group * a.N + n, sum);
+}
+
+// dA, dD and the bias's gradient from the sums of the chunks.
+__global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunks, float *__restrict__ dA, float *__restrict__ dD, float *__restrict__ dbias)
+{
+    const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.N;
+    const float *from;
+    float *to;
+    int64_t at, stride;
+    if (i < each) { from = a.part_a; to = dA; at = i; stride = each; }
+    else if (i < each + a.channels) { from = a.part_d; to = dD; at = i - each; stride = a.channels; }
+    else if (i < each + 2 * (int64_t)a.channels) { from = a.part_bias; to = dbias; at = i - each - a.channels; stride = a.channels; }
+    else return;
+    if (!to) return;
+    float sum = 0.f;
+    for (int c = 0; c < chunks; ++c) sum += from[c * stride + at];
+    to[at] = sum;
+}
+
+struct BwdBytes {
+    size_t carry, a, d, bc;
+    size_t all() const { return carry + a + 2 * d + bc; }
+};
+
+BwdBytes bytes_of(const sn_scan_shape &s, const ScanPlan &p)
+{
+    BwdBytes b;
+    b.carry = scan_carry_bytes(s, p);
+    b.a = align_up((size_t)p.chunks * s.channels * s.states * 4, 256);
+    b.d = align_up((size_t)p.chunks * s.channels * 4, 256);
+    b.bc = align_up((size_t)p.blocks * s.rows * 8 * p.NL * 4, 256);
+    return b;
+}
+
+}  // namespace
+
+void scan_bwd_bytes(const sn_scan_shape &s, size_t *min_bytes, size_t *preferred_bytes)
+{
+    *min_bytes = bytes_of(s, scan_plan(s, 1)).all();
+    *preferred_bytes = bytes_of(s, scan_plan(s, scan_parts_wanted(s, true))).all();
+}
+
+hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias,
+                           const ScanGrads &g, const sn_scan_shape &s, const int32_t *off, const float *h0, const float *states, void *ws, size_t ws_bytes, hipStream_t st)
+{
+    const size_t replay = states ? 0 : scan_states_bytes(s);
+    ScanPlan p = scan_plan(s, scan_parts_wanted(s, true));
+    while (p.parts > 1 && replay + bytes_of(s, p).all() > ws_bytes) p = scan_plan(s, p.parts - 1);
+    const BwdBytes b = bytes_of(s, p);
+    ScanArgs a = scan_args(s, p, off);
+    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.bias = bias; a.h0 = h0;
+    a.dy = g.dy; a.du = g.du; a.ddt = g.ddt; a.dB = g.dB; a.dC = g.dC; a.dz = g.dz; a.dhT = g.dhT; a.dh0 = g.dh0;
+    a.whole_u = scan_whole_rows(u, s.ld_u, s, p); a.whole_dt = scan_whole_rows(dt, s.ld_dt, s, p); a.whole_y = scan_whole_rows(g.dy, s.ld_y, s, p);
+    a.whole_du = scan_whole_rows(g.du, s.ld_du, s, p); a.whole_ddt = scan_whole_rows(g.ddt, s.ld_ddt, s, p);
+    a.whole_z = z && scan_whole_rows(z, s.ld_z, s, p); a.whole_dz = z && scan_whole_rows(g.dz, s.ld_dz, s, p);
+    char *at = (char *)ws;
+    a.states = states ? const_cast<float *>(states) : (float *)at;
+    at += replay;
+    if (p.parts > 1) scan_set_carry(a, s, p, at);
+    at += b.carry;
+    a.part_a = (float *)at; at += b.a;
+    a.part_d = (float *)at; at += b.d;
+    a.part_bias = (float *)at; at += b.d;
+    a.part_bc = (float *)at;
+    hipError_t e = hipSuccess;
+    if (!states && s.rows) e = launch_scan_states(a, s, p, st);
+    if (e != hipSuccess) return e;
+    const bool bf16 = s.dtype == SN_BF16;
+    e = by_lanes(p.NL, [&](auto NL) {
+        const dim3 grid(p.chunks, p.blocks);
+        if (p.parts > 1) {
+            if (bf16) scan_bwd_local_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a);
+            else scan_bwd_local_kernel<float, NL.value><<<grid, THREADS, 0, st>>>(a);
+            hipError_t f = hipGetLastError();
+            if (f == hipSuccess) f = launch_scan_carry(a, p, true, st);
+            if (f != hipSuccess) return f;
+        }
+        if (bf16) scan_bwd_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a);
+        else scan_bwd_kernel<float, NL.value><<<grid, THREADS, 0, st>>>(a);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    if (s.rows) {
+        const int64_t n = s.rows * s.groups * 8 * p.NL;
+        const unsigned blocks = (unsigned)((n + THREADS - 1) / THREADS);
+        if (bf16) scan_join_kernel<bf16_t><<<blocks, THREADS, 0, st>>>(a, s.groups, 4 * p.NL);
+        else scan_join_kernel<float><<<blocks, THREADS, 0, st>>>(a, s.groups, 4 * p.NL);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const int64_t n = (int64_t)s.channels * (s.states + 2);
+    scan_sum_kernel<<<(unsigned)((n + THREADS - 1) / THREADS), THREADS, 0, st>>>(a, p.chunks, g.dA, g.dD, g.ddt_bias);
+    return hipGetLastError();
+}
+
+}  // namespace sn
