@@ -93,7 +93,22 @@ __device__ inline void seq_forward(const SeqRows &r, SeqAt &a, int row)
     }
 }
 
-__device__ inline float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+// The instructions for 2^x, log2 x and 1 / x, each within one unit of the last place; e^x and log through them.  For |x| up to 20 the product with
+// log2(e) adds 20 * 2^-24 to the relative error of e^x.  2^x below 2^-126 is 0.
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float exp_fast(float x) { return exp2_fast(x * 1.44269504088896340736f); }
+__device__ inline float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
+__device__ inline float sigmoid(float x) { return rcp_fast(1.f + exp_fast(-x)); }
+
+// log(1 + e^x).  log(u) for u = 1 + e^x as rounded, times e^x / (u - 1), which takes the rounding of u out again to first order (u - 1 is
+// exact); from 20 on log(1 + e^-x) is below half a step of x.
+__device__ inline float softplus(float x)
+{
+    const float e = exp_fast(x), u = 1.f + e, d = u - 1.f;
+    const float l = __builtin_amdgcn_logf(u) * 0.69314718055994530942f;
+    const float r = d == 0.f ? e : l * (e * rcp_fast(d));
+    return x > 20.f ? x : r;
+}
 
 // a slot index of a step call: row -> slot, or -1 for a row to skip
 __device__ inline int step_slot(const int32_t *slots, int row, int num_slots)

@@ -1,9 +1,10 @@
 // What the scan's kernels share.
 //
 // A workgroup of four waves works on CB channels of one group and walks along the tokens in tiles of TS rows.  A lane holds four states of
-// one channel: NL lanes (2, 4, 8 or 16 for up to 8, 16, 32, 64 states) hold a channel's, the wave 64 / NL channels.  Sums over a channel's
-// states then are four products in a lane and log2(NL) exchanges, shared by NL rows (scatter_high); sums over channels, which only
-// the gradients of B and C need, are exchanges among the 64 / NL lanes of a wave, shared by as many values (scatter_low).
+// one channel: NL neighbouring lanes (2, 4, 8 or 16 for up to 8, 16, 32, 64 states) hold a channel's, the wave 64 / NL channels.  Sums
+// over a channel's states then are four products in a lane and log2(NL) exchanges, shared by NL rows; sums over channels, which only the
+// gradients of B and C need, are exchanges among the lanes of like states, shared by 64 / NL values (scatter_sum).  The latter are the
+// more, so they have the bits of the lane number that exchange in two instructions a pair and not three.
 // Rows are staged through LDS by all threads: delta, delta * u and the rest of what is per row and channel is computed once, not in every
 // lane of a channel.
 #pragma once
@@ -35,66 +36,78 @@ struct ScanArgs {
     int whole_u, whole_dt, whole_z, whole_y, whole_du, whole_ddt, whole_dz;
 };
 
-// Whether a tile's rows are in a sequence, its first or its last, a bit each; and the sequence, lane i's for row i.
-struct TileAt {
-    unsigned valid, start, end;
-    int seq;
-    __device__ int of(int i) const { return __shfl(seq, i, 64); }
+// The rows p0 .. p1 - 1 that one turn of a kernel's loop works on: those of one sequence in the tile of rows t0 .. t0 + TS - 1.  The tile's other
+// rows are staged as zeros: delta = 0 leaves the states, and the gradient on its way through them, as they are.
+struct Piece {
+    int t0, p0, p1, seq;
+    bool any, start, end;   // whether there is one; it begins, ends its sequence
+    __device__ bool holds(int row) const { return any && row >= p0 && row < p1; }
+    __device__ bool full() const { return p1 - p0 == TS; }
 };
-
-// The tile of rows t0 .. r1 - 1 at most.  `at`: the place of some row near it, whose sequence most tiles lie in.
-__device__ inline TileAt tile_at(const SeqRows &r, SeqAt &at, int t0, int r1, bool keep_last)
+// The first piece at or behind row `from` of the chunk r0 .. r1 - 1.  `at`: the place of an earlier row.
+__device__ inline Piece piece_from(const SeqRows &r, SeqAt &at, int from, int r0, int r1)
 {
-    const int last = min(t0 + TS, r1), lane = threadIdx.x & 63;
-    TileAt m;
-    if (at.s >= 0 && at.s < r.seqs && at.begin <= t0 && last <= at.end) {
-        m.valid = (1u << (last - t0)) - 1u;
-        m.start = t0 == at.begin;
-        m.end = last == at.end ? 1u << (last - t0 - 1) : 0u;
-        m.seq = at.s;
-        return m;
+    Piece p = {};
+    if (at.s < 0 && from < r1) at = seq_clamped(r, 0);
+    from = max(from, at.begin);
+    seq_forward(r, at, from);
+    from = max(from, at.begin);
+    if (at.s >= r.seqs || from >= r1 || from >= at.end) return p;
+    p.any = true;
+    p.seq = at.s;
+    p.p0 = from;
+    p.t0 = r0 + (from - r0) / TS * TS;
+    p.p1 = min(min(p.t0 + TS, at.end), r1);
+    p.start = from == at.begin;
+    p.end = p.p1 == at.end;
+    return p;
+}
+// The last piece in front of row `to`.  `at`: the place of a later row.
+__device__ inline Piece piece_before(const SeqRows &r, SeqAt &at, int to, int r0)
+{
+    Piece p = {};
+    if (at.s >= r.seqs && to > r0) at = seq_clamped(r, r.seqs - 1);
+    to = min(to, at.end);
+    while (at.s >= 0 && to > r0 && to <= at.begin) {
+        if (!r.off) return p;   // equal lengths: a chunk lies in one sequence
+        at = at.s ? seq_clamped(r, at.s - 1) : SeqAt{-1, 0, 0};
+        to = min(to, at.end);
     }
-    const int row = t0 + lane;
-    SeqAt mine = at;
-    bool in = false;
-    if (row < last) {
-        mine = seq_find(r, row);
-        in = mine.holds(row, r);
-    }
-    m.valid = (unsigned)__ballot(in);
-    m.start = (unsigned)__ballot(in && row == mine.begin);
-    m.end = (unsigned)__ballot(in && row == mine.end - 1);
-    m.seq = mine.s;
-    const int from = keep_last ? last - t0 - 1 : 0;
-    at.s = __builtin_amdgcn_readlane(mine.s, from);
-    at.begin = __builtin_amdgcn_readlane(mine.begin, from);
-    at.end = __builtin_amdgcn_readlane(mine.end, from);
-    return m;
+    if (at.s < 0 || to <= r0) return p;
+    p.any = true;
+    p.seq = at.s;
+    p.p1 = to;
+    p.t0 = r0 + (to - 1 - r0) / TS * TS;
+    p.p0 = max(p.t0, at.begin);
+    p.start = p.p0 == at.begin;
+    p.end = to == at.end;
+    return p;
 }
 
-// a[lane < 32], b[lane >= 32] with their partners' added: one swap and one addition for two values
-__device__ inline float fold32(float a, float b)
+// Lanes are numbered so that every bit of the number can be flipped by one cross-lane operand: bits 5 and 4 by the lane swaps, 3 by row_ror:8,
+// 1 and 0 by quad_perm.  For bit 2 there is only the mirror among eight lanes, which flips bits 1 and 0 of the hardware's
+// number as well; these two are therefore counted inverted where bit 2 is set.
+__device__ inline int scan_lane()
 {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const int lane = threadIdx.x & 63;
+    return lane & 4 ? lane ^ 3 : lane;
 }
-// the same for lanes 16 apart
-__device__ inline float fold16(float a, float b)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-template <int M> __device__ inline float fold_low(float a, float b)
-{
-    const bool up = (threadIdx.x & M) != 0;
-    const float keep = up ? b : a, give = up ? a : b;
-    return keep + __shfl_xor(give, M, 64);
-}
+
+// Of two values the one that belongs to this lane's bit M (a: clear, b: set), with the other lane's added.
 template <int M> __device__ inline float fold(float a, float b)
 {
-    if constexpr (M == 32) return fold32(a, b);
-    else if constexpr (M == 16) return fold16(a, b);
-    else return fold_low<M>(a, b);
+    if constexpr (M == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else {
+        constexpr int how = M == 8 ? 0x128 /* row_ror:8 */ : M == 4 ? 0x141 /* row_half_mirror */ : M == 2 ? 0x4e /* quad_perm:[2,3,0,1] */ : 0xb1 /* quad_perm:[1,0,3,2] */;
+        const bool up = (scan_lane() & M) != 0;
+        const float keep = up ? b : a, give = up ? a : b;
+        return keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), how, 0xf, 0xf, true));
+    }
 }
 
 // v[i] summed over the lanes that differ in the bits from TOP down to LOW; the lane whose bits there read i gets sum i.
@@ -113,10 +126,6 @@ template <int TOP, int LOW, int COUNT> __device__ inline float scatter_sum(float
     }
 }
 
-__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32; results below 2^-126 are 0
-
-__device__ inline float softplus(float x) { return x > 20.f ? x : log1pf(expf(x)); }   // log(1 + e^-20) is below half a step of 20
-
 // The lane's channel of a group's block, its states, and what is fixed of them.
 template <int NL> struct ScanLane {
     int c, n0, channel;   // channel within the workgroup's, first state, channel of the tensors
@@ -124,14 +133,26 @@ template <int NL> struct ScanLane {
     float A2[4];          // A * log2(e)
     __device__ ScanLane(const ScanArgs &a, int c0, int nch)
     {
-        constexpr int CW = ScanGeo<NL>::CW;
-        const int lane = threadIdx.x & 63;
-        c = (threadIdx.x / 64) * CW + lane % CW;
-        n0 = lane / CW * 4;
+        const int lane = scan_lane();
+        c = (threadIdx.x / 64) * ScanGeo<NL>::CW + lane / NL;
+        n0 = lane % NL * 4;
         there = c < nch;
         channel = c0 + c;
 #pragma unroll
         for (int i = 0; i < 4; ++i) A2[i] = there && n0 + i < a.N ? a.A[(int64_t)channel * a.N + n0 + i] * 1.44269504088896340736f : 0.f;
+    }
+    // the same for the library's own arrays, whose rows of states are aligned where N is a multiple of 4
+    __device__ void load_own(const float *p, int64_t k, const ScanArgs &a, float (&v)[4]) const
+    {
+        if (a.N % 4) return load(p, k, a, v);
+        float4 q = {0.f, 0.f, 0.f, 0.f};
+        if (there && n0 < a.N) q = *reinterpret_cast<const float4 *>(p + (k * a.channels + channel) * a.N + n0);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    }
+    __device__ void store_own(float *p, int64_t k, const ScanArgs &a, const float (&v)[4]) const
+    {
+        if (a.N % 4) return store(p, k, a, v);
+        if (there && n0 < a.N) *reinterpret_cast<float4 *>(p + (k * a.channels + channel) * a.N + n0) = make_float4(v[0], v[1], v[2], v[3]);
     }
     // four states of array p, [..][channels][N], at index k of its first dimension
     __device__ void load(const float *p, int64_t k, const ScanArgs &a, float (&v)[4]) const
@@ -176,12 +197,12 @@ template <typename T, int NL> struct Staged {
 template <typename T, int NL> struct StagedBC {
     static constexpr int COUNT = TS * ScanGeo<NL>::NP, PER = (COUNT + 255) / 256;
     T v[PER];
-    __device__ void load(const void *base, int64_t ld, int t0, int64_t column, int N, unsigned valid)
+    __device__ void load(const void *base, int64_t ld, const Piece &p, int64_t column, int N)
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int k = i * 256 + threadIdx.x, row = k / ScanGeo<NL>::NP, n = k % ScanGeo<NL>::NP;
-            v[i] = k < COUNT && n < N && (valid >> row & 1) ? ((const T *)base)[(int64_t)(t0 + row) * ld + column + n] : (T)0;
+            v[i] = k < COUNT && n < N && p.holds(p.t0 + row) ? ((const T *)base)[(int64_t)(p.t0 + row) * ld + column + n] : (T)0;
         }
     }
     __device__ void put(float *lds) const

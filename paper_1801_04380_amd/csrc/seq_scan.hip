@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
     const int c0 = group * a.per_group + inside, nch = min(CB, a.per_group - inside);
     const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
     const ScanLane<NL> lane(a, c0, nch);
-    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = (threadIdx.x & 63) / G::CW;
+    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = scan_lane() % NL;
 
     float bias[VE], skip[VE];
 #pragma unroll
@@ -42,26 +42,26 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
     }
     float h[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
     bool crossed = false;
-    if (!LOCAL && part > 0) lane.load(a.carry, chunk, a, h);
+    if (!LOCAL && part > 0) lane.load_own(a.carry, chunk, a, h);
 
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, r0);
-        TileAt m = tile_at(a.rows, at, r0, r1, true);
+        Piece next = piece_from(a.rows, at, r0, r0, r1);
         Staged<T, NL> u, dt, z;
         StagedBC<T, NL> B, C;
-        const auto fetch = [&](int t0) {
-            const bool in = m.valid >> row & 1;
-            const int64_t t = t0 + row;
-            const int n = in ? nco : 0;
+        const auto fetch = [&]() {
+            const int64_t t = next.t0 + row;
+            const int n = next.holds((int)t) ? nco : 0;
             u.load(a.u, t * a.ld_u + c0 + co, n, a.whole_u);
             dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
             if (OUT && a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
-            B.load(a.B, a.ld_b, t0, (int64_t)group * a.N, a.N, m.valid);
-            if (OUT) C.load(a.C, a.ld_c, t0, (int64_t)group * a.N, a.N, m.valid);
+            B.load(a.B, a.ld_b, next, (int64_t)group * a.N, a.N);
+            if (OUT) C.load(a.C, a.ld_c, next, (int64_t)group * a.N, a.N);
         };
-        fetch(r0);
-        for (int t0 = r0; t0 < r1; t0 += TS) {
-            const bool in = m.valid >> row & 1;
+        if (next.any) fetch();
+        while (next.any) {
+            const Piece now = next;
+            const bool in = now.holds(now.t0 + row);
             float uu[VE], gate[VE];
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
@@ -74,71 +74,57 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
             }
             B.put(s_B);
             if (OUT) C.put(s_C);
-            const TileAt now = m;
             __syncthreads();
-            if (t0 + TS < r1) {
-                m = tile_at(a.rows, at, t0 + TS, r1, true);
-                fetch(t0 + TS);
-            }
-            if (!LOCAL && a.states) lane.store(a.states, (int64_t)span * a.tiles_per_span + (t0 - span * a.span_rows) / TS, a, h);
-
-            float acc[NL];
-            const auto step = [&](int t) {
-                const float delta = s_delta[t][lane.c], x = s_x[t][lane.c];
-                const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
-                float4 c = {};
-                if (OUT) c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    h[i] = fmaf(exp2_fast(delta * lane.A2[i]), h[i], x * bb[i]);
-                    sum = fmaf(h[i], cc[i], sum);
-                }
-                acc[t % NL] = sum;
-                if (LOCAL) sum_delta += delta;
-            };
-            const auto reset = [&](int t) {
+            next = piece_from(a.rows, at, now.p1, r0, r1);
+            if (next.any) fetch();
+            if (now.start) {
                 crossed = true;
                 sum_delta = 0.f;
-                if (a.h0) lane.load(a.h0, now.of(t), a, h);
+                if (a.h0) lane.load(a.h0, now.seq, a, h);
                 else h[0] = h[1] = h[2] = h[3] = 0.f;
-            };
-            const auto flush = [&](int t) {   // rows t + 1 - NL .. t are done
-                if (OUT) s_y[t / NL * NL + nl][lane.c] = scatter_sum<32, G::CW>(acc);
-            };
-            if (!(now.start & ~1u) && !(now.end & (now.end - 1))) {
-                // one sequence; rows behind its end leave h as it is
-                if (now.start) reset(0);
-#pragma unroll
-                for (int t = 0; t < TS; ++t) {
-                    step(t);
-                    if (t % NL == NL - 1) flush(t);
-                }
-                if (OUT && a.hT && now.end) lane.store(a.hT, now.of(__builtin_ctz(now.end)), a, h);
-            } else {
-                for (int tb = 0; tb < TS; tb += NL) {
-#pragma unroll
-                    for (int i = 0; i < NL; ++i) {
-                        const int t = tb + i;
-                        if (now.start >> t & 1) reset(t);
-                        step(t);
-                        if (OUT && a.hT && (now.end >> t & 1)) lane.store(a.hT, now.of(t), a, h);
-                    }
-                    flush(tb + NL - 1);
-                }
+            } else if (!LOCAL && a.states && now.p0 == now.t0) {
+                lane.store_own(a.states, (int64_t)span * a.tiles_per_span + (now.t0 - span * a.span_rows) / TS, a, h);
             }
+
+            const auto rows = [&](int tb) {   // NL rows, and the sums of their outputs
+                float acc[NL];
+#pragma unroll
+                for (int k = 0; k < NL; ++k) {
+                    const int t = tb + k;
+                    const float delta = s_delta[t][lane.c], x = s_x[t][lane.c];
+                    const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
+                    float4 c = {};
+                    if (OUT) c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                    const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        h[i] = fmaf(exp2_fast(delta * lane.A2[i]), h[i], x * bb[i]);
+                        sum = fmaf(h[i], cc[i], sum);
+                    }
+                    acc[k] = sum;
+                    if (LOCAL) sum_delta += delta;
+                }
+                if (OUT) s_y[tb + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
+            };
+            if (now.full()) {
+#pragma unroll
+                for (int tb = 0; tb < TS; tb += NL) rows(tb);
+            } else {
+                for (int tb = (now.p0 - now.t0) / NL * NL; tb < now.p1 - now.t0; tb += NL) rows(tb);
+            }
+            if (OUT && a.hT && now.end) lane.store(a.hT, now.seq, a, h);
             __syncthreads();
             if (OUT && in) {
                 Staged<T, NL> y;
 #pragma unroll
                 for (int i = 0; i < VE; ++i) y.set(i, fmaf(skip[i], uu[i], s_y[row][co + i]) * gate[i]);
-                y.store(a.y, (int64_t)(t0 + row) * a.ld_y + c0 + co, nco, a.whole_y);
+                y.store(a.y, (int64_t)(now.t0 + row) * a.ld_y + c0 + co, nco, a.whole_y);
             }
         }
     }
     if (LOCAL) {
-        lane.store(a.carry, chunk, a, h);
+        lane.store_own(a.carry, chunk, a, h);
         if (lane.n0 == 0 && lane.there) a.sum_delta[(int64_t)chunk * a.channels + lane.channel] = sum_delta;
         if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
     }
@@ -196,7 +182,7 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (n0 + i >= a.N) continue;
-        const float h = fmaf(expf(delta * A[i]), from[i], delta * u * seq_ld<T>(B + i));
+        const float h = fmaf(exp_fast(delta * A[i]), from[i], delta * u * seq_ld<T>(B + i));
         sum = fmaf(h, seq_ld<T>(C + i), sum);
         to[i] = h;
     }

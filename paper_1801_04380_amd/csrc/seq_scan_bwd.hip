@@ -39,19 +39,21 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     float g[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
     bool crossed = false;
     SeqAt at = seq_find(a.rows, r1 - 1);
-    const int last = r0 + (r1 - 1 - r0) / TS * TS;
-    for (int t0 = last; t0 >= r0; t0 -= TS) {
-        const TileAt m = tile_at(a.rows, at, t0, r1, false);
-        const bool in = m.valid >> row & 1;
-        const int n = in ? nco : 0;
-        const int64_t t = t0 + row;
-        Staged<T, NL> dt, z, dy;
-        StagedBC<T, NL> C;
+    Piece next = piece_before(a.rows, at, r1, r0);
+    Staged<T, NL> dt, z, dy;
+    StagedBC<T, NL> C;
+    const auto fetch = [&]() {
+        const int64_t t = next.t0 + row;
+        const int n = next.holds((int)t) ? nco : 0;
         dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
         dy.load(a.dy, t * a.ld_y + c0 + co, n, a.whole_y);
         if (a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
-        C.load(a.C, a.ld_c, t0, (int64_t)group * a.N, a.N, m.valid);
-        __syncthreads();
+        C.load(a.C, a.ld_c, next, (int64_t)group * a.N, a.N);
+    };
+    if (next.any) fetch();
+    while (next.any) {
+        const Piece now = next;
+        const bool in = now.holds(now.t0 + row);
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
             const float raw = dt.get(i) + bias[i];
@@ -60,33 +62,44 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
         }
         C.put(s_C);
         __syncthreads();
-#pragma unroll
-        for (int k = TS - 1; k >= 0; --k) {
-            if (m.end >> k & 1) {
-                crossed = true;
-                sum_delta = 0.f;
-                if (a.dhT) lane.load(a.dhT, m.of(k), a, g);
-                else g[0] = g[1] = g[2] = g[3] = 0.f;
-            }
-            const float delta = s_delta[k][lane.c], gy = s_g[k][lane.c];
-            const float4 c = *reinterpret_cast<const float4 *>(&s_C[k * NP + lane.n0]);
-            const float cc[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] = exp2_fast(delta * lane.A2[i]) * fmaf(gy, cc[i], g[i]);
-            sum_delta += delta;
+        next = piece_before(a.rows, at, now.p0, r0);
+        if (next.any) fetch();
+        if (now.end) {
+            crossed = true;
+            sum_delta = 0.f;
+            if (a.dhT) lane.load(a.dhT, now.seq, a, g);
+            else g[0] = g[1] = g[2] = g[3] = 0.f;
         }
+        const auto rows = [&](int tb) {
+#pragma unroll
+            for (int k = 3; k >= 0; --k) {
+                const float delta = s_delta[tb + k][lane.c], gy = s_g[tb + k][lane.c];
+                const float4 c = *reinterpret_cast<const float4 *>(&s_C[(tb + k) * NP + lane.n0]);
+                const float cc[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g[i] = exp2_fast(delta * lane.A2[i]) * fmaf(gy, cc[i], g[i]);
+                sum_delta += delta;
+            }
+        };
+        if (now.full()) {
+#pragma unroll
+            for (int tb = TS - 4; tb >= 0; tb -= 4) rows(tb);
+        } else {
+            for (int tb = (now.p1 - 1 - now.t0) / 4 * 4; tb >= 0 && tb + 3 >= now.p0 - now.t0; tb -= 4) rows(tb);
+        }
+        __syncthreads();
     }
-    lane.store(a.carry, chunk, a, g);
+    lane.store_own(a.carry, chunk, a, g);
     if (lane.n0 == 0 && lane.there) a.sum_delta[(int64_t)chunk * a.channels + lane.channel] = sum_delta;
     if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
 }
 
 template <typename T, int NL>
-__global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanArgs a)
+__global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
     constexpr int CB = G::CB, NP = G::NP, VE = G::VE, CW = G::CW;
-    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_g[TS][CB], s_y[TS][CB];
+    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_g[TS][CB], s_y[TS][CB], s_gb[TS][CB], s_qa[TS][CB];
     __shared__ alignas(16) float s_B[TS * NP], s_C[TS * NP];
     __shared__ float s_bc[4][TS][2 * NP];
 
@@ -95,7 +108,7 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanArgs a)
     const int c0 = group * a.per_group + inside, nch = min(CB, a.per_group - inside);
     const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
     const ScanLane<NL> lane(a, c0, nch);
-    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = (threadIdx.x & 63) / CW, wave = threadIdx.x / 64;
+    const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = scan_lane() % NL, wave = threadIdx.x / 64;
     float bias[VE], skip[VE], dD[VE], dbias[VE], A[4], dA[4];
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
@@ -109,146 +122,165 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanArgs a)
         dA[i] = 0.f;
     }
     float g[4] = {0.f, 0.f, 0.f, 0.f};
-    if (part < a.parts - 1) lane.load(a.carry, chunk, a, g);
+    if (part < a.parts - 1) lane.load_own(a.carry, chunk, a, g);
 
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, r1 - 1);
-        const int last = r0 + (r1 - 1 - r0) / TS * TS;
-        TileAt m = tile_at(a.rows, at, last, r1, false);
+        Piece next = piece_before(a.rows, at, r1, r0);
         Staged<T, NL> u, dt, z, dy;
         StagedBC<T, NL> B, C;
-        const auto fetch = [&](int t0) {
-            const int64_t t = t0 + row;
-            const int n = m.valid >> row & 1 ? nco : 0;
+        const auto fetch = [&]() {
+            const int64_t t = next.t0 + row;
+            const int n = next.holds((int)t) ? nco : 0;
             u.load(a.u, t * a.ld_u + c0 + co, n, a.whole_u);
             dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
             dy.load(a.dy, t * a.ld_y + c0 + co, n, a.whole_y);
             if (a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
-            B.load(a.B, a.ld_b, t0, (int64_t)group * a.N, a.N, m.valid);
-            C.load(a.C, a.ld_c, t0, (int64_t)group * a.N, a.N, m.valid);
+            B.load(a.B, a.ld_b, next, (int64_t)group * a.N, a.N);
+            C.load(a.C, a.ld_c, next, (int64_t)group * a.N, a.N);
         };
-        fetch(last);
-        for (int t0 = last; t0 >= r0; t0 -= TS) {
-            const bool in = m.valid >> row & 1;
-            float uu[VE], raw[VE], delta[VE], gy[VE], dyv[VE], zz[VE];
+        if (next.any) fetch();
+        while (next.any) {
+            const Piece now = next;
+            const bool in = now.holds(now.t0 + row);
+            Staged<T, NL> u0 = u, dt0 = dt, z0 = z, dy0 = dy;   // as loaded: what is made of them is in LDS, or made again
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                raw[i] = dt.get(i) + bias[i];
-                delta[i] = in && i < nco ? (a.softplus ? softplus(raw[i]) : raw[i]) : 0.f;
-                uu[i] = u.get(i);
-                dyv[i] = dy.get(i);
-                zz[i] = a.z ? z.get(i) : 0.f;
-                gy[i] = a.z ? dyv[i] * zz[i] * sigmoid(zz[i]) : dyv[i];
-                s_delta[row][co + i] = delta[i];
-                s_x[row][co + i] = delta[i] * uu[i];
-                s_g[row][co + i] = gy[i];
+                const float raw = dt.get(i) + bias[i], delta = in && i < nco ? (a.softplus ? softplus(raw) : raw) : 0.f;
+                s_delta[row][co + i] = delta;
+                s_x[row][co + i] = delta * u.get(i);
+                s_g[row][co + i] = a.z ? dy.get(i) * (z.get(i) * sigmoid(z.get(i))) : dy.get(i);
             }
             B.put(s_B);
             C.put(s_C);
-            const TileAt now = m;
             __syncthreads();
-            if (t0 - TS >= r0) {
-                m = tile_at(a.rows, at, t0 - TS, r1, false);
-                fetch(t0 - TS);
+            float first[4];   // the state in front of the piece
+            if (!now.start) lane.load_own(a.states, (int64_t)span * a.tiles_per_span + (now.t0 - span * a.span_rows) / TS, a, first);
+            else if (a.h0) lane.load(a.h0, now.seq, a, first);
+            else first[0] = first[1] = first[2] = first[3] = 0.f;
+            next = piece_before(a.rows, at, now.p0, r0);
+            if (next.any) fetch();
+            if (now.end) {
+                if (a.dhT) lane.load(a.dhT, now.seq, a, g);
+                else g[0] = g[1] = g[2] = g[3] = 0.f;
             }
 
-            // the states of the tile, forwards
-            float hs[TS][4], decay[TS][4], first[4], acc[NL];
-            const bool one = !(now.start & ~1u) && !(now.end & (now.end - 1));
-            if (now.start & 1) {
-                if (a.h0) lane.load(a.h0, now.of(0), a, first);
-                else first[0] = first[1] = first[2] = first[3] = 0.f;
-            } else {
-                lane.load(a.states, (int64_t)span * a.tiles_per_span + (t0 - span * a.span_rows) / TS, a, first);
-            }
+            constexpr int TB = CW < 8 ? 1 : CW / 8;       // rows whose 8 values share the exchanges over channels
+            constexpr int GR = NL > TB ? NL : TB;         // rows that are worked on or left out together
+            constexpr int HR = GR > 8 ? GR : 8;           // rows whose states are in registers at a time
+            const auto tile = [&](auto whole) {
+                constexpr bool WHOLE = whole.value;
+                const auto outside = [&](int tb, int n) { return !WHOLE && (now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1); };
+                // the state in front of the second half
+                float mid[4] = {first[0], first[1], first[2], first[3]};
+                if constexpr (HR < TS) {
+                    if (!outside(0, HR))
 #pragma unroll
-            for (int t = 0; t < TS; ++t) {
-                const float d = s_delta[t][lane.c], x = s_x[t][lane.c];
-                const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
-                float past[4], sum = 0.f;
+                        for (int t = 0; t < HR; ++t) {
+                            const float d = s_delta[t][lane.c], x = s_x[t][lane.c];
+                            const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
+                            const float bb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) past[i] = t ? hs[t ? t - 1 : 0][i] : first[i];
-                if (!one && t && (now.start >> t & 1)) {
-                    if (a.h0) lane.load(a.h0, now.of(t), a, past);
-                    else past[0] = past[1] = past[2] = past[3] = 0.f;
+                            for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(d * lane.A2[i]), mid[i], x * bb[i]);
+                        }
                 }
+#pragma unroll 1
+                for (int half = TS - HR; half >= 0; half -= HR) {
+                    float hs[HR + 1][4], decay[HR][4];   // hs[k]: the state in front of the half's row k
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    decay[t][i] = exp2_fast(d * lane.A2[i]);
-                    hs[t][i] = fmaf(decay[t][i], past[i], x * bb[i]);
-                    sum = fmaf(hs[t][i], cc[i], sum);
-                }
-                acc[t % NL] = sum;
-                if (t % NL == NL - 1) {
-                    const float y = scatter_sum<32, CW>(acc);
-                    if (a.z) s_y[t / NL * NL + nl][lane.c] = y;
-                }
-            }
-            // and its gradients, backwards
-            float gb[NL], qa[NL], bc[CW < 8 ? 8 : CW];
+                    for (int i = 0; i < 4; ++i) hs[0][i] = half ? mid[i] : first[i];
+                    // the states, forwards
 #pragma unroll
-            for (int t = TS - 1; t >= 0; --t) {
-                if (now.end >> t & 1) {
-                    if (a.dhT) lane.load(a.dhT, now.of(t), a, g);
-                    else g[0] = g[1] = g[2] = g[3] = 0.f;
-                }
-                const float d = s_delta[t][lane.c], x = s_x[t][lane.c], gyt = s_g[t][lane.c];
-                const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
-                float past[4], sum_b = 0.f, sum_a = 0.f;
+                    for (int kb = 0; kb < HR; kb += GR) {
+                        if (outside(half + kb, GR)) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) past[i] = t ? hs[t ? t - 1 : 0][i] : first[i];
-                if (!one && t && (now.start >> t & 1)) {
-                    if (a.h0) lane.load(a.h0, now.of(t), a, past);
-                    else past[0] = past[1] = past[2] = past[3] = 0.f;
-                }
-                constexpr int TB = CW < 8 ? 1 : CW / 8;   // rows whose 8 values share the exchanges over channels
+                            for (int k = kb; k < kb + GR; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float gi = fmaf(gyt, cc[i], g[i]);
-                    bc[t % TB * 8 + i] = gi * x;
-                    bc[t % TB * 8 + 4 + i] = gyt * hs[t][i];
-                    sum_b = fmaf(gi, bb[i], sum_b);
-                    g[i] = decay[t][i] * gi;
-                    const float q = g[i] * past[i];
-                    sum_a = fmaf(q, A[i], sum_a);
-                    dA[i] = fmaf(q, d, dA[i]);
-                }
-                if (a.dh0 && (now.start >> t & 1)) lane.store(a.dh0, now.of(t), a, g);
-                gb[t % NL] = sum_b;
-                qa[t % NL] = sum_a;
-                if (t % NL == 0) {   // rows t .. t + NL - 1 are done: their places take the sums
-                    const float vb = scatter_sum<32, CW>(gb), va = scatter_sum<32, CW>(qa);
-                    s_x[t + nl][lane.c] = vb;
-                    s_delta[t + nl][lane.c] = va;
-                }
-                if (t % TB == 0) {
-                    const int low = threadIdx.x & (CW - 1);
-                    if constexpr (CW >= 8) {
-                        const float v = scatter_sum<CW / 2, 1>(bc);
-                        s_bc[wave][t + low / 8][(low / 4 & 1) * NP + lane.n0 + low % 4] = v;
-                    } else {
-                        float lo[4] = {bc[0], bc[1], bc[2], bc[3]}, hi[4] = {bc[4], bc[5], bc[6], bc[7]};
-                        s_bc[wave][t][lane.n0 + low] = scatter_sum<2, 1>(lo);
-                        s_bc[wave][t][NP + lane.n0 + low] = scatter_sum<2, 1>(hi);
+                                for (int i = 0; i < 4; ++i) {
+                                    hs[k + 1][i] = hs[k][i];
+                                    decay[k][i] = 1.f;
+                                }
+                            continue;
+                        }
+                        float acc[NL];
+#pragma unroll
+                        for (int k = kb; k < kb + GR; ++k) {
+                            const int t = half + k;
+                            const float d = s_delta[t][lane.c], x = s_x[t][lane.c];
+                            const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                            const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                            float sum = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                decay[k][i] = exp2_fast(d * lane.A2[i]);
+                                hs[k + 1][i] = fmaf(decay[k][i], hs[k][i], x * bb[i]);
+                                sum = fmaf(hs[k + 1][i], cc[i], sum);
+                            }
+                            acc[t % NL] = sum;
+                            if (t % NL == NL - 1) s_y[t / NL * NL + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
+                        }
+                    }
+                    // and the gradients, backwards; what the rows' operands took in registers is read again
+                    asm volatile("" ::: "memory");
+#pragma unroll
+                    for (int kb = HR - GR; kb >= 0; kb -= GR) {
+                        if (outside(half + kb, GR)) continue;
+                        float gb[NL], qa[NL], bc[8 * TB];
+#pragma unroll
+                        for (int k = kb + GR - 1; k >= kb; --k) {
+                            const int t = half + k;
+                            const float d = s_delta[t][lane.c], x = s_x[t][lane.c], gyt = s_g[t][lane.c];
+                            const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                            const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                            float sum_b = 0.f, sum_a = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float gi = fmaf(gyt, cc[i], g[i]);
+                                bc[t % TB * 8 + i] = gi * x;
+                                bc[t % TB * 8 + 4 + i] = gyt * hs[k + 1][i];
+                                sum_b = fmaf(gi, bb[i], sum_b);
+                                g[i] = decay[k][i] * gi;
+                                const float q = g[i] * hs[k][i];
+                                sum_a = fmaf(q, A[i], sum_a);
+                                dA[i] = fmaf(q, d, dA[i]);
+                            }
+                            gb[t % NL] = sum_b;
+                            qa[t % NL] = sum_a;
+                            if (t % NL == 0) {   // rows t .. t + NL - 1 are done
+                                s_gb[t + nl][lane.c] = scatter_sum<NL / 2, 1>(gb);
+                                s_qa[t + nl][lane.c] = scatter_sum<NL / 2, 1>(qa);
+                            }
+                            if (t % TB == 0) {
+                                const int k8 = scan_lane() / NL;   // which of the rows' values this lane gets
+                                if constexpr (CW >= 8) {
+                                    s_bc[wave][t + k8 / 8][(k8 / 4 & 1) * NP + lane.n0 + k8 % 4] = scatter_sum<32, NL>(bc);
+                                } else {
+                                    float lo[4] = {bc[0], bc[1], bc[2], bc[3]}, hi[4] = {bc[4], bc[5], bc[6], bc[7]};
+                                    s_bc[wave][t][lane.n0 + k8] = scatter_sum<32, NL>(lo);
+                                    s_bc[wave][t][NP + lane.n0 + k8] = scatter_sum<32, NL>(hi);
+                                }
+                            }
+                        }
                     }
                 }
-            }
+            };
+            if (now.full()) tile(ScanInt<1>());
+            else tile(ScanInt<0>());
+            if (a.dh0 && now.start) lane.store(a.dh0, now.seq, a, g);
             __syncthreads();
             if (in) {
-                const int64_t t = t0 + row;
+                const int64_t t = now.t0 + row;
                 Staged<T, NL> o;
                 float dd[VE];
 #pragma unroll
                 for (int i = 0; i < VE; ++i) {
-                    const float vb = s_x[row][co + i], va = s_delta[row][co + i];
-                    o.set(i, fmaf(gy[i], skip[i], delta[i] * vb));
-                    dd[i] = fmaf(uu[i], vb, va);
-                    if (a.softplus) dd[i] *= sigmoid(raw[i]);
+                    const float vb = s_gb[row][co + i], va = s_qa[row][co + i], gy = s_g[row][co + i], uu = u0.get(i);
+                    o.set(i, fmaf(gy, skip[i], s_delta[row][co + i] * vb));
+                    dd[i] = fmaf(uu, vb, va);
+                    if (a.softplus) dd[i] *= sigmoid(dt0.get(i) + bias[i]);
                     if (i < nco) {
                         dbias[i] += dd[i];
-                        dD[i] = fmaf(gy[i], uu[i], dD[i]);
+                        dD[i] = fmaf(gy, uu, dD[i]);
                     }
                 }
                 o.store(a.du, t * a.ld_du + c0 + co, nco, a.whole_du);
@@ -258,21 +290,21 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_kernel(ScanArgs a)
                 if (a.z) {
 #pragma unroll
                     for (int i = 0; i < VE; ++i) {
-                        const float s = sigmoid(zz[i]);
-                        o.set(i, dyv[i] * fmaf(skip[i], uu[i], s_y[row][co + i]) * s * (1.f + zz[i] * (1.f - s)));
+                        const float zz = z0.get(i), s = sigmoid(zz);
+                        o.set(i, dy0.get(i) * fmaf(skip[i], u0.get(i), s_y[row][co + i]) * s * (1.f + zz * (1.f - s)));
                     }
                     o.store(a.dz, t * a.ld_dz + c0 + co, nco, a.whole_dz);
                 }
             }
             for (int k = threadIdx.x; k < TS * 2 * NP; k += THREADS) {
                 const int r = k / (2 * NP), n = k % (2 * NP);
-                if (now.valid >> r & 1)
-                    a.part_bc[((int64_t)blockIdx.y * a.rows.rows + t0 + r) * (2 * NP) + n] = s_bc[0][r][n] + s_bc[1][r][n] + s_bc[2][r][n] + s_bc[3][r][n];
+                if (now.holds(now.t0 + r))
+                    a.part_bc[((int64_t)blockIdx.y * a.rows.rows + now.t0 + r) * (2 * NP) + n] = s_bc[0][r][n] + s_bc[1][r][n] + s_bc[2][r][n] + s_bc[3][r][n];
             }
             __syncthreads();
         }
     }
-    lane.store(a.part_a, chunk, a, dA);
+    lane.store_own(a.part_a, chunk, a, dA);
     // dD and the bias's gradient: over the 16 threads that stage a channel
     for (int what = 0; what < 2; ++what) {
         __syncthreads();
