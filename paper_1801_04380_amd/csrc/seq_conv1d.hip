@@ -42,6 +42,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
                                                              int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, bool whole_x,
                                                              bool whole_y, const T *__restrict__ state_in, T *__restrict__ state_out)
 {
+    constexpr int R = 8;   // rows at a time: their loads are all on their way before the first is used
     const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V, n = channels - c;
     if (n <= 0) return;
     Taps<T, V, W> taps;
@@ -49,23 +50,53 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
     if (r0 < r1) {
         SeqAt at = seq_find(rows, r0);
-        for (int t = r0; t < r1; ++t) {
-            seq_forward(rows, at, t);
-            if (!at.holds(t, rows)) continue;
-            Pack<T, V> in[W], out;
+        Pack<T, V> in[W - 1 + R];   // the rows in front, if the last turn was a whole one, and this turn's
+        bool have = false;
+        for (int b = r0; b < r1; b += R) {
+            seq_forward(rows, at, b);
+            if (at.holds(b, rows) && b - (W - 1) >= at.begin && b + R <= min(at.end, r1) && !(state_out && b + R == at.end)) {
+                if (!have)
 #pragma unroll
-            for (int j = 0; j < W; ++j) in[j] = tap_input<T, V>(x, ld_x, state_in, channels, W, at, t - (W - 1) + j, c, n, whole_x);
+                    for (int j = 0; j < W - 1; ++j) in[j].load(x + (int64_t)(b - (W - 1) + j) * ld_x + c, n, whole_x);
+                have = true;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float p = taps.b[i];
+                for (int k = 0; k < R; ++k) in[W - 1 + k].load(x + (int64_t)(b + k) * ld_x + c, n, whole_x);
 #pragma unroll
-                for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[j].get(i), p);
-                out.set(i, silu ? p * sigmoid(p) : p);
+                for (int k = 0; k < R; ++k) {
+                    Pack<T, V> out;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float p = taps.b[i];
+#pragma unroll
+                        for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[k + j].get(i), p);
+                        out.set(i, silu ? p * sigmoid(p) : p);
+                    }
+                    out.store(y + (int64_t)(b + k) * ld_y + c, n, whole_y);
+                }
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j) in[j] = in[R + j];
+                continue;
             }
-            out.store(y + (int64_t)t * ld_y + c, n, whole_y);
-            if (state_out && t == at.end - 1)
+            // a sequence begins or ends here: row by row
+            have = false;
+            for (int t = b; t < min(b + R, r1); ++t) {
+                seq_forward(rows, at, t);
+                if (!at.holds(t, rows)) continue;
+                Pack<T, V> tap[W], out;
 #pragma unroll
-                for (int j = 1; j < W; ++j) in[j].store(state_out + ((int64_t)at.s * (W - 1) + j - 1) * channels + c, n, false);
+                for (int j = 0; j < W; ++j) tap[j] = tap_input<T, V>(x, ld_x, state_in, channels, W, at, t - (W - 1) + j, c, n, whole_x);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float p = taps.b[i];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], tap[j].get(i), p);
+                    out.set(i, silu ? p * sigmoid(p) : p);
+                }
+                out.store(y + (int64_t)t * ld_y + c, n, whole_y);
+                if (state_out && t == at.end - 1)
+#pragma unroll
+                    for (int j = 1; j < W; ++j) tap[j].store(state_out + ((int64_t)at.s * (W - 1) + j - 1) * channels + c, n, false);
+            }
         }
     }
     // the states of empty sequences pass through
@@ -115,13 +146,17 @@ __device__ inline void gradient_of_p(const T *x, const T *dy, const T *state, in
     }
 }
 
-// part[slice][W + 1][channels]: the slice's sums for dw, then for dbias
+// part[slice][W + 1][channels]: the slice's sums for dw, then for dbias.
+// A thread walks down the rows r0 .. r1 - 1 of its slice, R at a time.  A turn at b reads x and dy of the rows b + W - 1 .. b + R + W - 2,
+// makes their dp, and with the W - 1 rows in front, which it has, dx of rows b .. b + R - 1.  The first turn, at r0 - R, only fills what the next
+// one takes over; R >= 2 (W - 1) rows make that complete.
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, const T *__restrict__ dy,
                                                              T *__restrict__ dx, float *__restrict__ part, int channels, int silu, int64_t ld_x, int64_t ld_y,
                                                              int64_t ld_dx, SeqRows rows, int run, bool whole_x, bool whole_y, bool whole_dx,
                                                              const T *__restrict__ state_in, const T *__restrict__ dstate_out)
 {
+    constexpr int R = W <= 5 ? 8 : 16, H = W - 1;
     const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V, n = channels - c;
     if (n <= 0) return;
     Taps<T, V, W> taps;
@@ -129,42 +164,115 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
     float dw[V][W] = {}, db[V] = {};
     if (r0 < r1) {
-        SeqAt at = seq_find(rows, r0);
-        for (int t = r0; t < r1; ++t) {
-            seq_forward(rows, at, t);
-            if (!at.holds(t, rows)) continue;
-            float dp[V], g[V] = {};
-            Pack<T, V> in[W], other[W], out;
+        float in[H + R][V] = {}, dp[H + R][V] = {};   // x and dp of rows b .. b + R + H - 1
+        SeqAt lead = seq_find(rows, max(r0 - R + H, 0)), trail = seq_find(rows, r0);
+        for (int b = r0 - R; b < r1; b += R) {
+            Pack<T, V> xs[R], gs[R];
 #pragma unroll
-            for (int k = W - 1; k >= 0; --k) {
-                if (t + k >= at.end) continue;
-                gradient_of_p<T, V, W>(x, dy, state_in, channels, silu, ld_x, ld_y, rows, at, t + k, c, n, whole_x, whole_y, taps, dp, k == 0 ? in : other);
+            for (int k = 0; k < R; ++k) {
+                const int t = b + H + k;
+                const int m = t >= 0 && t < rows.rows ? n : 0;
+                xs[k].load(x + (int64_t)t * ld_x + c, m, whole_x);
+                gs[k].load(dy + (int64_t)t * ld_y + c, m, whole_y);
+            }
+            if (b >= r0) seq_forward(rows, trail, b);
+            const bool plain = b >= r0 && b + H + R <= min(trail.end, r1) && trail.holds(b, rows);
 #pragma unroll
-                for (int i = 0; i < V; ++i) g[i] = fmaf(taps.w[i][W - 1 - k], dp[i], g[i]);
+            for (int k = 0; k < R; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) in[H + k][i] = xs[k].get(i);
+            if (plain) {
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float p = taps.b[i], d = gs[k].get(i);
+                        if (silu) {
+#pragma unroll
+                            for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[k + j][i], p);
+                            d *= silu_slope(p);
+                        }
+                        dp[H + k][i] = d;
+                        db[i] += d;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) dw[i][j] = fmaf(d, in[k + j][i], dw[i][j]);
+                    }
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    Pack<T, V> out;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float g = 0.f;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) g = fmaf(taps.w[i][H - j], dp[k + j][i], g);
+                        out.set(i, g);
+                    }
+                    out.store(dx + (int64_t)(b + k) * ld_dx + c, n, whole_dx);
+                }
+            } else {
+                // the slice's or a sequence's first or last rows are among these
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    const int t = b + H + k;
+                    const bool mine = t >= r0 && t < r1;
+                    seq_forward(rows, lead, t);
+                    const bool there = t >= 0 && lead.holds(t, rows);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float tap[W], p = taps.b[i], d = there ? gs[k].get(i) : 0.f;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) {
+                            const int src = t - H + j;
+                            tap[j] = src >= lead.begin ? in[k + j][i] : 0.f;
+                            if (there && src < lead.begin && state_in && i < n)
+                                tap[j] = seq_ld<T>(state_in + ((int64_t)lead.s * H + H + src - lead.begin) * channels + c + i);
+                            p = fmaf(taps.w[i][j], tap[j], p);
+                        }
+                        if (silu) d = there ? d * silu_slope(p) : 0.f;
+                        dp[H + k][i] = d;
+                        if (there && mine) {
+                            db[i] += d;
+#pragma unroll
+                            for (int j = 0; j < W; ++j) dw[i][j] = fmaf(d, tap[j], dw[i][j]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    const int t = b + k;
+                    if (t < r0 || t >= r1) continue;
+                    seq_forward(rows, trail, t);
+                    if (!trail.holds(t, rows)) continue;
+                    Pack<T, V> out;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float g = 0.f;
+#pragma unroll
+                        for (int j = 0; j < W; ++j)
+                            if (t + j < trail.end) g = fmaf(taps.w[i][H - j], dp[k + j][i], g);
+                        if (dstate_out && t >= trail.end - H && i < n) g += seq_ld<T>(dstate_out + ((int64_t)trail.s * H + t - (trail.end - H)) * channels + c + i);
+                        out.set(i, g);
+                    }
+                    out.store(dx + (int64_t)t * ld_dx + c, n, whole_dx);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                db[i] += dp[i];
+            for (int j = 0; j < H; ++j)
 #pragma unroll
-                for (int j = 0; j < W; ++j) dw[i][j] = fmaf(dp[i], in[j].get(i), dw[i][j]);
-            }
-            if (dstate_out && t >= at.end - (W - 1))
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (i < n) g[i] += seq_ld<T>(dstate_out + ((int64_t)at.s * (W - 1) + t - (at.end - (W - 1))) * channels + c + i);
-#pragma unroll
-            for (int i = 0; i < V; ++i) out.set(i, g[i]);
-            out.store(dx + (int64_t)t * ld_dx + c, n, whole_dx);
+                for (int i = 0; i < V; ++i) {
+                    in[j][i] = in[R + j][i];
+                    dp[j][i] = dp[R + j][i];
+                }
         }
     }
     float *to = part + (size_t)blockIdx.y * (W + 1) * channels + c;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i < n) {
+    for (int j = 0; j <= W; ++j) {
+        Pack<float, V> v;
 #pragma unroll
-            for (int j = 0; j < W; ++j) to[(size_t)j * channels + i] = dw[i][j];
-            to[(size_t)W * channels + i] = db[i];
-        }
+        for (int i = 0; i < V; ++i) v.e[i] = j < W ? dw[i][j < W ? j : 0] : db[i];
+        v.store(to + (size_t)j * channels, n, channels % V == 0);
+    }
 }
 
 // The gradient of the initial states: one thread per sequence and channel.
@@ -203,12 +311,21 @@ __global__ void __launch_bounds__(THREADS) conv1d_dstate_kernel(const T *__restr
     }
 }
 
+// dw and dbias from the slices' sums: 16 threads along the slices of each value, joined in a fixed order.
 __global__ void __launch_bounds__(THREADS) conv1d_sum_kernel(const float *__restrict__ part, float *__restrict__ dw, float *__restrict__ dbias, int channels, int width, int slices)
 {
-    const int c = blockIdx.x * THREADS + threadIdx.x, j = blockIdx.y;
-    if (c >= channels) return;
+    __shared__ float sums[16][16];
+    const int lane = threadIdx.x / 16, c = blockIdx.x * 16 + threadIdx.x % 16, j = blockIdx.y;
     float sum = 0.f;
-    for (int s = 0; s < slices; ++s) sum += part[((size_t)s * (width + 1) + j) * channels + c];
+    if (c < channels)
+#pragma unroll 8
+        for (int s = lane; s < slices; s += 16) sum += part[((size_t)s * (width + 1) + j) * channels + c];
+    sums[lane][threadIdx.x % 16] = sum;
+    __syncthreads();
+    if (lane || c >= channels) return;
+    sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < 16; ++s) sum += sums[s][threadIdx.x];
     if (j < width) dw[(size_t)c * width + j] = sum;
     else if (dbias) dbias[c] = sum;
 }
@@ -284,14 +401,24 @@ template <typename T> hipError_t fwd(const void *x, const void *w, const float *
     });
 }
 
-int bwd_blocks(int channels) { return div_up(channels, 4 * THREADS); }   // the fp32 count, the larger: the scratch does not depend on the type
+constexpr int BWD_V = 4;   // channels of a thread: with 8 the windows of x and dp alone would take 176 registers
+
+int bwd_blocks(int channels) { return div_up(channels, BWD_V * THREADS); }
+
+// Rows of a slice: about 512 workgroups, two waves a SIMD, of 64 rows at least, beside which the turn that fills the windows costs little.
+int bwd_run(int64_t rows, int channels)
+{
+    const int64_t want = (512 + bwd_blocks(channels) - 1) / bwd_blocks(channels);
+    const int64_t run = ((rows + want - 1) / want + 15) / 16 * 16;
+    return (int)(run < 64 ? 64 : run);
+}
 
 template <typename T> hipError_t bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
                                      const int32_t *off, const void *state_in, const void *dstate_out, void *dstate_in, void *scratch, hipStream_t st)
 {
-    constexpr int V = vec_of<T>();
+    constexpr int V = BWD_V;
     return by_width(s.width, [&](auto W) {
-        const int run = run_of(s.rows, bwd_blocks(s.channels)), slices = s.rows ? div_up(s.rows, run) : 1;
+        const int run = bwd_run(s.rows, s.channels), slices = s.rows ? div_up(s.rows, run) : 1;
         const SeqRows rows = rows_of(s, off);
         conv1d_bwd_kernel<T, V, W.value><<<dim3(div_up(s.channels, V * THREADS), slices), THREADS, 0, st>>>(
             (const T *)x, (const T *)w, bias, (const T *)dy, (T *)dx, (float *)scratch, s.channels, s.silu, s.ld_x, s.ld_y, s.ld_dx, rows, run,
@@ -299,7 +426,7 @@ template <typename T> hipError_t bwd(const void *x, const void *w, const float *
             (const T *)dstate_out);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        conv1d_sum_kernel<<<dim3(div_up(s.channels, THREADS), s.width + 1), THREADS, 0, st>>>((const float *)scratch, dw, dbias, s.channels, s.width, slices);
+        conv1d_sum_kernel<<<dim3(div_up(s.channels, 16), s.width + 1), THREADS, 0, st>>>((const float *)scratch, dw, dbias, s.channels, s.width, slices);
         e = hipGetLastError();
         if (e != hipSuccess || !dstate_in || s.width == 1) return e;
         conv1d_dstate_kernel<T, W.value><<<dim3(s.seqs, div_up(s.channels, THREADS)), THREADS, 0, st>>>(
@@ -331,7 +458,7 @@ hipError_t launch_conv1d_fwd(const void *x, const void *w, const float *bias, vo
 
 size_t conv1d_scratch_bytes(int64_t rows, int channels, int width)
 {
-    const int slices = rows ? div_up(rows, run_of(rows, bwd_blocks(channels))) : 1;
+    const int slices = rows ? div_up(rows, bwd_run(rows, channels)) : 1;
     return align_up((size_t)slices * (width + 1) * channels * 4, 256);
 }
 

@@ -3,8 +3,8 @@
 // A dozen operations per element against two (backward: three) tensors read and written: bound by HBM.  A lane holds `unit`s of 2 E
 // elements: the E pairs (i, i + rot/2) or (2i, 2i+1) of neighbouring angles, both halves in the same lane, so that the rotation exchanges
 // nothing; behind rot_dim a unit is 2 E neighbours that are not turned.  LPH lanes (a power of two) hold a head, a wave 64 / LPH
-// heads of one row at a time, NU units a lane.  The wave then takes the row's next heads, q's and k's in one list, with the same
-// angles: they are formed once per row, in 64 bits.
+// heads of one row at a time, NU units a lane.  The wave then takes the row's next heads, q's and k's in one list, loading the next ones
+// before it works on these.  A row's angles are formed once, one by each lane, in 64 bits, and handed round through LDS.
 #include "seq.h"
 
 namespace sn {
@@ -17,29 +17,33 @@ struct HeadArgs {
     float eps;
 };
 
-template <typename T, int E> struct Unit {
-    float a[E], b[E];
-    // whole: both halves on E elements' alignment
+template <typename T, int E> struct Raw {   // a unit as it lies in memory
+    Pack<T, E> lo, hi;
+    __device__ void zero()
+    {
+        lo.zero();
+        hi.zero();
+    }
     __device__ void load(const T *head, int pa, int pb, int nb, bool pairs)
     {
-        if (pairs) {  // a, b alternate: 2 E neighbours from pa on
-            Pack<T, E> lo, hi;
-            lo.load(head + pa, E, true);
-            hi.load(head + pa + E, E, true);
+        lo.load(head + pa, E, true);
+        if (pairs) hi.load(head + pa + E, E, true);
+        else if (nb) hi.load(head + pb, E, true);
+        else hi.zero();
+    }
+};
+
+template <typename T, int E> struct Unit {
+    float a[E], b[E];
+    __device__ Unit() {}
+    __device__ Unit(const Raw<T, E> &r, bool pairs)
+    {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                a[i] = 2 * i < E ? lo.get(2 * i < E ? 2 * i : 0) : hi.get(2 * i < E ? 0 : 2 * i - E);
-                b[i] = 2 * i + 1 < E ? lo.get(2 * i + 1 < E ? 2 * i + 1 : 0) : hi.get(2 * i + 1 < E ? 0 : 2 * i + 1 - E);
-            }
-        } else {
-            Pack<T, E> v;
-            v.load(head + pa, E, true);
-#pragma unroll
-            for (int i = 0; i < E; ++i) a[i] = v.get(i);
-            v.zero();
-            if (nb) v.load(head + pb, E, true);
-#pragma unroll
-            for (int i = 0; i < E; ++i) b[i] = v.get(i);
+        for (int i = 0; i < E; ++i) {   // pairs: a, b alternate through the 2 E neighbours
+            const float ea = 2 * i < E ? r.lo.get(2 * i < E ? 2 * i : 0) : r.hi.get(2 * i < E ? 0 : 2 * i - E);
+            const float eb = 2 * i + 1 < E ? r.lo.get(2 * i + 1 < E ? 2 * i + 1 : 0) : r.hi.get(2 * i + 1 < E ? 0 : 2 * i + 1 - E);
+            a[i] = pairs ? ea : r.lo.get(i);
+            b[i] = pairs ? eb : r.hi.get(i);
         }
     }
     __device__ void store(T *head, int pa, int pb, int nb, bool pairs) const
@@ -115,50 +119,69 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
                                                            int64_t ld_gk, int64_t ld_oq, int64_t ld_ok)
 {
     constexpr int HPW = 64 / LPH;
+    __shared__ float turn[WAVES][2][SN_HEADNORM_MAX_DIM / 2];   // of the wave's row
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, group = lane / LPH, l = lane % LPH;
     const int parts = gridDim.y;                       // the list of heads is cut into so many parts
     const int per = ((h.heads + HPW - 1) / HPW + parts - 1) / parts * HPW;
-    const int h0 = blockIdx.y * per, h1 = min(h.heads, h0 + per);
+    const int h0 = blockIdx.y * per, h1 = min(h.heads, h0 + per), stride = gridDim.x * WAVES;
     float dw[2][BWD ? NU : 1][BWD ? E : 1][2] = {};
-    for (int row = blockIdx.x * WAVES + wave; row < h.rows; row += gridDim.x * WAVES) {
+
+    const auto pick = [&](const T *pq, const T *pk, int64_t lq, int64_t lk, int row, int head) {
+        return head < h.q_heads ? pq + (int64_t)row * lq + (int64_t)head * h.head_dim : pk + (int64_t)row * lk + (int64_t)(head - h.q_heads) * h.head_dim;
+    };
+    Raw<T, E> rx[NU], rg[BWD ? NU : 1];
+    const auto fetch = [&](int row, int head) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            const Place<E> p(u * LPH + l, h);
+            if (row < h.rows && head < h1 && p.there) {
+                rx[u].load(pick(q, k, ld_q, ld_k, row, head), p.pa, p.pb, p.nb, p.pairs);
+                if (BWD) rg[u].load(pick(gq, gk, ld_gq, ld_gk, row, head), p.pa, p.pb, p.nb, p.pairs);
+            } else {
+                rx[u].zero();
+                if (BWD) rg[u].zero();
+            }
+        }
+    };
+    int row = blockIdx.x * WAVES + wave;
+    fetch(row, h0 + group);
+    for (; row < h.rows; row += stride) {
         const int pos = positions ? positions[row] : row;
+        for (int i = lane; i < h.rot_dim / 2; i += 64) {
+            float c, s;
+            turn_of(pos, freq[i], c, s);
+            turn[wave][0][i] = c;
+            turn[wave][1][i] = s;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // a wave's own writes, read by its other lanes
         float co[NU][E], si[NU][E];
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             const Place<E> p(u * LPH + l, h);
+            const bool turned = p.there && p.angle >= 0;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                co[u][i] = 1.f;
-                si[u][i] = 0.f;
-                if (p.there && p.angle >= 0) turn_of(pos, freq[p.angle + i], co[u][i], si[u][i]);
+                co[u][i] = turned ? turn[wave][0][turned ? p.angle + i : 0] : 1.f;
+                si[u][i] = turned ? turn[wave][1][turned ? p.angle + i : 0] : 0.f;
             }
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next row's are written
         for (int head = h0 + group; head < h1 + group; head += HPW) {   // every lane goes round as often
             const bool here = head < h1, is_q = head < h.q_heads;
-            const int hd = is_q ? head : head - h.q_heads;
-            const T *x = (is_q ? q + (int64_t)row * ld_q : k + (int64_t)row * ld_k) + (int64_t)hd * h.head_dim;
-            const T *g = nullptr;
-            if (BWD) g = (is_q ? gq + (int64_t)row * ld_gq : gk + (int64_t)row * ld_gk) + (int64_t)hd * h.head_dim;
-            T *o = (is_q ? oq + (int64_t)row * ld_oq : ok + (int64_t)row * ld_ok) + (int64_t)hd * h.head_dim;
+            T *o = (is_q ? oq + (int64_t)row * ld_oq + (int64_t)head * h.head_dim : ok + (int64_t)row * ld_ok + (int64_t)(head - h.q_heads) * h.head_dim);
             const float *w = is_q ? (h.has_wq ? wq : nullptr) : (h.has_wk ? wk : nullptr);
             Unit<T, E> v[NU], d[BWD ? NU : 1];
             float sum = 0.f;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 const Place<E> p(u * LPH + l, h);
-                if (here && p.there) {
-                    v[u].load(x, p.pa, p.pb, p.nb, p.pairs);
-                    if (BWD) d[u].load(g, p.pa, p.pb, p.nb, p.pairs);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        v[u].a[i] = v[u].b[i] = 0.f;
-                        if (BWD) d[u].a[i] = d[u].b[i] = 0.f;
-                    }
-                }
+                v[u] = Unit<T, E>(rx[u], p.pairs);
+                if (BWD) d[u] = Unit<T, E>(rg[u], p.pairs);
 #pragma unroll
                 for (int i = 0; i < E; ++i) sum = fmaf(v[u].a[i], v[u].a[i], fmaf(v[u].b[i], v[u].b[i], sum));
             }
+            const bool more = head - group + HPW < h1;
+            fetch(more ? row : row + stride, more ? head + HPW : h0 + group);
             const float r = 1.f / sqrtf(head_sum<LPH>(sum) / (float)h.head_dim + h.eps);
             if (!BWD) {
 #pragma unroll
@@ -235,20 +258,21 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
     }
 }
 
-// One workgroup per 16 elements of the two weights' gradients: 16 threads along the workgroups' sums, joined in a fixed order.
-__global__ void __launch_bounds__(THREADS) headnorm_sum_kernel(const float *__restrict__ part, float *__restrict__ dwq, float *__restrict__ dwk, int head_dim, int parts)
+// One workgroup per 16 elements of the two weights' gradients: 64 threads along the workgroups' sums, joined in a fixed order.
+__global__ void __launch_bounds__(1024) headnorm_sum_kernel(const float *__restrict__ part, float *__restrict__ dwq, float *__restrict__ dwk, int head_dim, int parts)
 {
     const int e = threadIdx.x % 16, lane = threadIdx.x / 16, i = blockIdx.x * 16 + e;
-    __shared__ float sums[16][16];
+    __shared__ float sums[64][16];
     float s = 0.f;
     if (i < 2 * head_dim)
-        for (int p = lane; p < parts; p += 16) s += part[(size_t)p * 2 * head_dim + i];
+#pragma unroll 8
+        for (int p = lane; p < parts; p += 64) s += part[(size_t)p * 2 * head_dim + i];
     sums[lane][e] = s;
     __syncthreads();
     if (lane || i >= 2 * head_dim) return;
     s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) s += sums[j][e];
+    for (int j = 0; j < 64; ++j) s += sums[j][e];
     if (i < head_dim) {
         if (dwq) dwq[i] = s;
     } else if (dwk) {
@@ -259,7 +283,7 @@ __global__ void __launch_bounds__(THREADS) headnorm_sum_kernel(const float *__re
 // How many workgroups walk the rows, and into how many parts the list of heads is cut: waves for the chip where rows are few.
 void grid_of(int64_t rows, int heads, dim3 *grid)
 {
-    int64_t blocks = (rows + WAVES - 1) / WAVES, most = 2048;
+    int64_t blocks = (rows + WAVES - 1) / WAVES, most = 1024;
     if (blocks > most) blocks = most;
     if (blocks < 1) blocks = 1;
     int64_t parts = 1024 / blocks;
@@ -352,7 +376,7 @@ hipError_t launch_headnorm_bwd(const void *q, const void *k, const float *wq, co
     if (e != hipSuccess || (!dwq && !dwk)) return e;
     dim3 grid;
     grid_of(s.rows, s.q_heads + s.k_heads, &grid);
-    headnorm_sum_kernel<<<(2 * s.head_dim + 15) / 16, THREADS, 0, st>>>((const float *)scratch, dwq, dwk, s.head_dim, (int)(grid.x * grid.y));
+    headnorm_sum_kernel<<<(2 * s.head_dim + 15) / 16, 1024, 0, st>>>((const float *)scratch, dwq, dwk, s.head_dim, (int)(grid.x * grid.y));
     return hipGetLastError();
 }
 
