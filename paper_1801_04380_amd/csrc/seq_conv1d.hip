@@ -17,11 +17,15 @@ template <typename T, int V, int W> struct Taps {
     float w[V][W], b[V];
     __device__ void load(const T *wp, const float *bp, int c, int n)
     {
+        Pack<T, V> raw[W];   // the V * W elements lie side by side
+        const bool whole = n >= V && reinterpret_cast<uintptr_t>(wp + (size_t)c * W) % (sizeof(T) * V) == 0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) raw[j].load(wp + (size_t)c * W + j * V, n * W - j * V, whole);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             b[i] = bp && i < n ? bp[c + i] : 0.f;
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[i][j] = i < n ? seq_ld<T>(wp + (size_t)(c + i) * W + j) : 0.f;
+            for (int j = 0; j < W; ++j) w[i][j] = raw[(i * W + j) / V].get((i * W + j) % V);
         }
     }
 };
@@ -380,12 +384,13 @@ SeqRows rows_of(const sn_conv1d_shape &s, const int32_t *off)
 
 int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// Rows of a workgroup's run, a multiple of 16: about 2048 workgroups of `per` channel blocks each, as long as the runs are 16 rows and more.
-int run_of(int64_t rows, int per)
+// Rows of a workgroup's run, a multiple of 16: about 512 workgroups over `blocks` channel blocks, two waves a SIMD, each with eight rows' loads on their
+// way; 32 rows at least, beside which the filters and the rows in front cost little.
+int run_of(int64_t rows, int blocks, int least)
 {
-    const int64_t want = (2048 + per - 1) / per;
+    const int64_t want = (512 + blocks - 1) / blocks;
     const int64_t run = ((rows + want - 1) / want + 15) / 16 * 16;
-    return (int)(run < 16 ? 16 : run);
+    return (int)(run < least ? least : run);
 }
 
 template <typename T> hipError_t fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off, const void *state_in,
@@ -393,7 +398,7 @@ template <typename T> hipError_t fwd(const void *x, const void *w, const float *
 {
     constexpr int V = vec_of<T>();
     return by_width(s.width, [&](auto W) {
-        const int blocks = div_up(s.channels, V * THREADS), run = run_of(s.rows, blocks);
+        const int blocks = div_up(s.channels, V * THREADS), run = run_of(s.rows, blocks, 32);
         conv1d_fwd_kernel<T, V, W.value><<<dim3(blocks, s.rows ? div_up(s.rows, run) : 1), THREADS, 0, st>>>(
             (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows_of(s, off), run, rows_aligned(x, s.ld_x, sizeof(T), V),
             rows_aligned(y, s.ld_y, sizeof(T), V), (const T *)state_in, (T *)state_out);
@@ -405,13 +410,8 @@ constexpr int BWD_V = 4;   // channels of a thread: with 8 the windows of x and 
 
 int bwd_blocks(int channels) { return div_up(channels, BWD_V * THREADS); }
 
-// Rows of a slice: about 512 workgroups, two waves a SIMD, of 64 rows at least, beside which the turn that fills the windows costs little.
-int bwd_run(int64_t rows, int channels)
-{
-    const int64_t want = (512 + bwd_blocks(channels) - 1) / bwd_blocks(channels);
-    const int64_t run = ((rows + want - 1) / want + 15) / 16 * 16;
-    return (int)(run < 64 ? 64 : run);
-}
+// Rows of a slice: 64 at least, beside which the turn that fills the windows costs little.
+int bwd_run(int64_t rows, int channels) { return run_of(rows, bwd_blocks(channels), 64); }
 
 template <typename T> hipError_t bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
                                      const int32_t *off, const void *state_in, const void *dstate_out, void *dstate_in, void *scratch, hipStream_t st)

@@ -3,17 +3,30 @@
 // A dozen operations per element against two (backward: three) tensors read and written: bound by HBM.  A lane holds `unit`s of 2 E
 // elements: the E pairs (i, i + rot/2) or (2i, 2i+1) of neighbouring angles, both halves in the same lane, so that the rotation exchanges
 // nothing; behind rot_dim a unit is 2 E neighbours that are not turned.  LPH lanes (a power of two) hold a head, a wave 64 / LPH
-// heads of one row at a time, NU units a lane.  The wave then takes the row's next heads, q's and k's in one list, loading the next ones
-// before it works on these.  A row's angles are formed once, one by each lane, in 64 bits, and handed round through LDS.
+// heads of one row at a time, NU units a lane.  The wave then takes the row's next heads, loading them before it works on these.  A workgroup
+// has to do with q or with k alone, whose weight its lanes hold.  A row's angles are formed once, one by each lane, in 64 bits, and handed
+// round through LDS.
 #include "seq.h"
+#include <type_traits>
 
 namespace sn {
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 
+struct HeadSide {   // q or k
+    const void *x, *g;
+    void *out;
+    const float *w;
+    int64_t ld_x, ld_g, ld_out;
+    int heads, parts;   // its list of heads is cut into so many parts
+};
 struct HeadArgs {
-    int rows, q_heads, heads, head_dim, rot_dim, interleaved, has_wq, has_wk;
+    HeadSide side[2];
+    const int32_t *positions;
+    const float *freq;
+    float *part;
+    int rows, head_dim, rot_dim, interleaved;
     float eps;
 };
 
@@ -105,38 +118,50 @@ __device__ inline void turn_of(int position, float freq, float &c, float &s)
     sincospif(2.f * part, &s, &c);
 }
 
+// The sum over the LPH lanes of a head, in each of them.  Within 16 lanes by the cross-lane operands of the addition: neighbours, pairs,
+// the mirror of four (whose four hold the same by then), eight apart.
 template <int LPH> __device__ inline float head_sum(float v)
 {
-#pragma unroll
-    for (int m = LPH / 2; m >= 1; m /= 2) v += __shfl_xor(v, m, 64);
+    const auto other = [](float x, auto how) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), how.value, 0xf, 0xf, true)); };
+    if constexpr (LPH >= 2) v += other(v, std::integral_constant<int, 0xb1>());    // quad_perm:[1,0,3,2]
+    if constexpr (LPH >= 4) v += other(v, std::integral_constant<int, 0x4e>());    // quad_perm:[2,3,0,1]
+    if constexpr (LPH >= 8) v += other(v, std::integral_constant<int, 0x141>());   // row_half_mirror
+    if constexpr (LPH >= 16) v += other(v, std::integral_constant<int, 0x128>());  // row_ror:8
+    if constexpr (LPH >= 32) v += __shfl_xor(v, 16, 64);
+    if constexpr (LPH >= 64) v += __shfl_xor(v, 32, 64);
     return v;
 }
 
 template <typename T, int E, int NU, int LPH, bool BWD>
-__global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *k, const float *__restrict__ wq, const float *__restrict__ wk,
-                                                           const int32_t *__restrict__ positions, const float *__restrict__ freq, const T *gq, const T *gk,
-                                                           T *oq, T *ok, float *__restrict__ part, HeadArgs h, int64_t ld_q, int64_t ld_k, int64_t ld_gq,
-                                                           int64_t ld_gk, int64_t ld_oq, int64_t ld_ok)
+__global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
 {
     constexpr int HPW = 64 / LPH;
     __shared__ float turn[WAVES][2][SN_HEADNORM_MAX_DIM / 2];   // of the wave's row
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, group = lane / LPH, l = lane % LPH;
-    const int parts = gridDim.y;                       // the list of heads is cut into so many parts
-    const int per = ((h.heads + HPW - 1) / HPW + parts - 1) / parts * HPW;
-    const int h0 = blockIdx.y * per, h1 = min(h.heads, h0 + per), stride = gridDim.x * WAVES;
-    float dw[2][BWD ? NU : 1][BWD ? E : 1][2] = {};
-
-    const auto pick = [&](const T *pq, const T *pk, int64_t lq, int64_t lk, int row, int head) {
-        return head < h.q_heads ? pq + (int64_t)row * lq + (int64_t)head * h.head_dim : pk + (int64_t)row * lk + (int64_t)(head - h.q_heads) * h.head_dim;
-    };
+    const bool is_q = (int)blockIdx.y < h.side[0].parts;
+    const HeadSide &s = h.side[is_q ? 0 : 1];
+    const int part = blockIdx.y - (is_q ? 0 : h.side[0].parts);
+    const int per = ((s.heads + HPW - 1) / HPW + s.parts - 1) / s.parts * HPW;
+    const int h0 = part * per, h1 = min(s.heads, h0 + per), stride = gridDim.x * WAVES;
+    const float inv_dim = 1.f / (float)h.head_dim;
+    float wa[NU][E], wb[NU][E], dw[BWD ? NU : 1][BWD ? E : 1][2] = {};
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        const Place<E> p(u * LPH + l, h);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            wa[u][i] = s.w && p.there ? s.w[p.at_a(i)] : 1.f;
+            wb[u][i] = s.w && p.there && p.nb ? s.w[p.at_b(i)] : 1.f;
+        }
+    }
     Raw<T, E> rx[NU], rg[BWD ? NU : 1];
     const auto fetch = [&](int row, int head) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             const Place<E> p(u * LPH + l, h);
             if (row < h.rows && head < h1 && p.there) {
-                rx[u].load(pick(q, k, ld_q, ld_k, row, head), p.pa, p.pb, p.nb, p.pairs);
-                if (BWD) rg[u].load(pick(gq, gk, ld_gq, ld_gk, row, head), p.pa, p.pb, p.nb, p.pairs);
+                rx[u].load((const T *)s.x + (int64_t)row * s.ld_x + (int64_t)head * h.head_dim, p.pa, p.pb, p.nb, p.pairs);
+                if (BWD) rg[u].load((const T *)s.g + (int64_t)row * s.ld_g + (int64_t)head * h.head_dim, p.pa, p.pb, p.nb, p.pairs);
             } else {
                 rx[u].zero();
                 if (BWD) rg[u].zero();
@@ -146,12 +171,12 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
     int row = blockIdx.x * WAVES + wave;
     fetch(row, h0 + group);
     for (; row < h.rows; row += stride) {
-        const int pos = positions ? positions[row] : row;
+        const int pos = h.positions ? h.positions[row] : row;
         for (int i = lane; i < h.rot_dim / 2; i += 64) {
-            float c, s;
-            turn_of(pos, freq[i], c, s);
+            float c, sn;
+            turn_of(pos, h.freq[i], c, sn);
             turn[wave][0][i] = c;
-            turn[wave][1][i] = s;
+            turn[wave][1][i] = sn;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // a wave's own writes, read by its other lanes
         float co[NU][E], si[NU][E];
@@ -166,10 +191,10 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next row's are written
-        for (int head = h0 + group; head < h1 + group; head += HPW) {   // every lane goes round as often
-            const bool here = head < h1, is_q = head < h.q_heads;
-            T *o = (is_q ? oq + (int64_t)row * ld_oq + (int64_t)head * h.head_dim : ok + (int64_t)row * ld_ok + (int64_t)(head - h.q_heads) * h.head_dim);
-            const float *w = is_q ? (h.has_wq ? wq : nullptr) : (h.has_wk ? wk : nullptr);
+        for (int hb = h0; hb < h1; hb += HPW) {
+            const int head = hb + group;
+            const bool here = head < h1;
+            T *o = (T *)s.out + (int64_t)row * s.ld_out + (int64_t)head * h.head_dim;
             Unit<T, E> v[NU], d[BWD ? NU : 1];
             float sum = 0.f;
 #pragma unroll
@@ -180,9 +205,9 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
 #pragma unroll
                 for (int i = 0; i < E; ++i) sum = fmaf(v[u].a[i], v[u].a[i], fmaf(v[u].b[i], v[u].b[i], sum));
             }
-            const bool more = head - group + HPW < h1;
+            const bool more = hb + HPW < h1;
             fetch(more ? row : row + stride, more ? head + HPW : h0 + group);
-            const float r = 1.f / sqrtf(head_sum<LPH>(sum) / (float)h.head_dim + h.eps);
+            const float r = __builtin_amdgcn_rsqf(fmaf(head_sum<LPH>(sum), inv_dim, h.eps));
             if (!BWD) {
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
@@ -190,7 +215,7 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
                     if (!here || !p.there) continue;
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        const float na = v[u].a[i] * r * (w ? w[p.at_a(i)] : 1.f), nb = v[u].b[i] * r * (w && p.nb ? w[p.at_b(i)] : 1.f);
+                        const float na = v[u].a[i] * r * wa[u][i], nb = v[u].b[i] * r * wb[u][i];
                         v[u].a[i] = na * co[u][i] - nb * si[u][i];
                         v[u].b[i] = nb * co[u][i] + na * si[u][i];
                     }
@@ -200,29 +225,27 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
                 float dot = 0.f;
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
-                    const Place<E> p(u * LPH + l, h);
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
                         const float ga = d[u].a[i] * co[u][i] + d[u].b[i] * si[u][i], gb = d[u].b[i] * co[u][i] - d[u].a[i] * si[u][i];
-                        const float xa = v[u].a[i] * r, xb = v[u].b[i] * r;
-                        dw[0][u][i][0] += is_q ? ga * xa : 0.f;
-                        dw[0][u][i][1] += is_q ? gb * xb : 0.f;
-                        dw[1][u][i][0] += is_q ? 0.f : ga * xa;
-                        dw[1][u][i][1] += is_q ? 0.f : gb * xb;
-                        d[u].a[i] = ga * (w && p.there ? w[p.at_a(i)] : 1.f);
-                        d[u].b[i] = gb * (w && p.there && p.nb ? w[p.at_b(i)] : 1.f);
-                        dot = fmaf(d[u].a[i], xa, fmaf(d[u].b[i], xb, dot));
+                        v[u].a[i] *= r;
+                        v[u].b[i] *= r;
+                        dw[u][i][0] = fmaf(ga, v[u].a[i], dw[u][i][0]);
+                        dw[u][i][1] = fmaf(gb, v[u].b[i], dw[u][i][1]);
+                        d[u].a[i] = ga * wa[u][i];
+                        d[u].b[i] = gb * wb[u][i];
+                        dot = fmaf(d[u].a[i], v[u].a[i], fmaf(d[u].b[i], v[u].b[i], dot));
                     }
                 }
-                dot = head_sum<LPH>(dot) / (float)h.head_dim;
+                dot = head_sum<LPH>(dot) * inv_dim;
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
                     const Place<E> p(u * LPH + l, h);
                     if (!here || !p.there) continue;
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        d[u].a[i] = r * (d[u].a[i] - v[u].a[i] * r * dot);
-                        d[u].b[i] = r * (d[u].b[i] - v[u].b[i] * r * dot);
+                        d[u].a[i] = r * fmaf(-dot, v[u].a[i], d[u].a[i]);
+                        d[u].b[i] = r * fmaf(-dot, v[u].b[i], d[u].b[i]);
                     }
                     d[u].store(o, p.pa, p.pb, p.nb, p.pairs);
                 }
@@ -230,66 +253,64 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(const T *q, const T *
         }
     }
     if (!BWD) return;
-    // the workgroup's sums for both weights: over the head groups of a wave, then over its waves
-    __shared__ float sums[WAVES][2][SN_HEADNORM_MAX_DIM];
+    // the workgroup's sums for its weight: over the head groups of a wave, then over its waves
+    __shared__ float sums[BWD ? WAVES : 1][BWD ? SN_HEADNORM_MAX_DIM : 1];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int u = 0; u < NU; ++u) {
+        const Place<E> p(u * LPH + l, h);
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const Place<E> p(u * LPH + l, h);
+        for (int i = 0; i < E; ++i)
 #pragma unroll
-            for (int i = 0; i < E; ++i)
+            for (int half = 0; half < 2; ++half) {
+                float v = dw[BWD ? u : 0][BWD ? i : 0][half];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float s = dw[m][BWD ? u : 0][BWD ? i : 0][half];
-#pragma unroll
-                    for (int x = LPH; x < 64; x *= 2) s += __shfl_xor(s, x, 64);
-                    if (group == 0 && p.there && (half == 0 || p.nb)) sums[wave][m][half ? p.at_b(i) : p.at_a(i)] = s;
-                }
-        }
+                for (int x = LPH; x < 64; x *= 2) v += __shfl_xor(v, x, 64);
+                if (group == 0 && p.there && (half == 0 || p.nb)) sums[BWD ? wave : 0][half ? p.at_b(i) : p.at_a(i)] = v;
+            }
+    }
     __syncthreads();
-    float *to = part + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * h.head_dim;
-    for (int i = threadIdx.x; i < 2 * h.head_dim; i += THREADS) {
-        const int m = i >= h.head_dim, e = m ? i - h.head_dim : i;
-        float s = 0.f;
+    float *to = h.part + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * h.head_dim;
+    for (int i = threadIdx.x; i < h.head_dim; i += THREADS) {
+        float v = 0.f;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) s += sums[v][m][e];
-        to[i] = s;
+        for (int x = 0; x < WAVES; ++x) v += sums[BWD ? x : 0][i];
+        to[i] = v;
     }
 }
 
-// One workgroup per 16 elements of the two weights' gradients: 64 threads along the workgroups' sums, joined in a fixed order.
-__global__ void __launch_bounds__(1024) headnorm_sum_kernel(const float *__restrict__ part, float *__restrict__ dwq, float *__restrict__ dwk, int head_dim, int parts)
+// One workgroup per 16 elements of a weight's gradient, y = 0 q's: 64 threads along the workgroups' sums, joined in a fixed order.
+__global__ void __launch_bounds__(1024) headnorm_sum_kernel(const float *__restrict__ part, float *__restrict__ dwq, float *__restrict__ dwk, int head_dim, int q_parts,
+                                                            int k_parts)
 {
-    const int e = threadIdx.x % 16, lane = threadIdx.x / 16, i = blockIdx.x * 16 + e;
+    const int e = threadIdx.x % 16, lane = threadIdx.x / 16, i = blockIdx.x * 16 + e, first = blockIdx.y ? q_parts : 0, count = blockIdx.y ? k_parts : q_parts;
     __shared__ float sums[64][16];
     float s = 0.f;
-    if (i < 2 * head_dim)
+    if (i < head_dim)
 #pragma unroll 8
-        for (int p = lane; p < parts; p += 64) s += part[(size_t)p * 2 * head_dim + i];
+        for (int p = lane; p < count; p += 64) s += part[(size_t)(first + p) * head_dim + i];
     sums[lane][e] = s;
     __syncthreads();
-    if (lane || i >= 2 * head_dim) return;
+    float *to = blockIdx.y ? dwk : dwq;
+    if (lane || i >= head_dim || !to) return;
     s = 0.f;
 #pragma unroll
     for (int j = 0; j < 64; ++j) s += sums[j][e];
-    if (i < head_dim) {
-        if (dwq) dwq[i] = s;
-    } else if (dwk) {
-        dwk[i - head_dim] = s;
-    }
+    to[i] = s;
 }
 
-// How many workgroups walk the rows, and into how many parts the list of heads is cut: waves for the chip where rows are few.
-void grid_of(int64_t rows, int heads, dim3 *grid)
+// How many workgroups walk the rows, and into how many parts the lists of heads are cut: waves for the chip where rows are few.
+struct HeadGrid {
+    int blocks, q_parts, k_parts;
+};
+HeadGrid grid_of(int64_t rows, int q_heads, int k_heads)
 {
-    int64_t blocks = (rows + WAVES - 1) / WAVES, most = 1024;
-    if (blocks > most) blocks = most;
-    if (blocks < 1) blocks = 1;
-    int64_t parts = 1024 / blocks;
-    if (parts > heads) parts = heads;
-    if (parts < 1) parts = 1;
-    *grid = dim3((unsigned)blocks, (unsigned)parts);
+    HeadGrid g;
+    const int64_t blocks = (rows + WAVES - 1) / WAVES;
+    g.blocks = (int)(blocks > 1024 ? 1024 : blocks < 1 ? 1 : blocks);
+    const int parts = 1024 / g.blocks;
+    g.q_parts = parts < q_heads ? parts : q_heads;
+    g.k_parts = parts < k_heads ? parts : k_heads;
+    return g;
 }
 
 template <int V> struct Is { static constexpr int value = V; };
@@ -324,29 +345,24 @@ int alignment(const void *p, int64_t ld, int esize)
     return v;
 }
 
-HeadArgs args_of(const sn_headnorm_shape &s, const float *wq, const float *wk)
-{
-    return {(int)s.rows, s.q_heads, s.q_heads + s.k_heads, s.head_dim, s.rot_dim, s.interleaved, wq != nullptr, wk != nullptr, s.eps};
-}
-
 int least(int a, int b) { return a < b ? a : b; }
 
 template <typename T, bool BWD>
 hipError_t launch(const void *q, const void *k, const float *wq, const float *wk, const int32_t *pos, const float *freq, const void *gq, const void *gk, void *oq,
                   void *ok, int64_t ld_gq, int64_t ld_gk, int64_t ld_oq, int64_t ld_ok, const sn_headnorm_shape &s, float *part, hipStream_t st)
 {
-    int al = least(alignment(q, s.ld_q, sizeof(T)), alignment(oq, ld_oq, sizeof(T)));
-    if (BWD) al = least(al, alignment(gq, ld_gq, sizeof(T)));
-    if (s.k_heads) {
-        al = least(al, least(alignment(k, s.ld_k, sizeof(T)), alignment(ok, ld_ok, sizeof(T))));
-        if (BWD) al = least(al, alignment(gk, ld_gk, sizeof(T)));
+    const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads);
+    const HeadArgs h = {{{q, gq, oq, wq, s.ld_q, ld_gq, ld_oq, s.q_heads, g.q_parts}, {k, gk, ok, wk, s.ld_k, ld_gk, ld_ok, s.k_heads, g.k_parts}}, pos, freq, part,
+                        (int)s.rows, s.head_dim, s.rot_dim, s.interleaved, s.eps};
+    int al = 16 / (int)sizeof(T);
+    for (const HeadSide &side : h.side) {
+        if (!side.heads) continue;
+        al = least(al, least(alignment(side.x, side.ld_x, sizeof(T)), alignment(side.out, side.ld_out, sizeof(T))));
+        if (BWD) al = least(al, alignment(side.g, side.ld_g, sizeof(T)));
     }
     while (s.head_dim % al) al /= 2;
-    dim3 grid;
-    grid_of(s.rows, s.q_heads + s.k_heads, &grid);
     return by_size<T>(s.head_dim, s.rot_dim, al, [&](auto E, auto NU, auto LPH) {
-        headnorm_kernel<T, E.value, NU.value, LPH.value, BWD><<<grid, THREADS, 0, st>>>((const T *)q, (const T *)k, wq, wk, pos, freq, (const T *)gq, (const T *)gk, (T *)oq,
-                                                                                        (T *)ok, part, args_of(s, wq, wk), s.ld_q, s.ld_k, ld_gq, ld_gk, ld_oq, ld_ok);
+        headnorm_kernel<T, E.value, NU.value, LPH.value, BWD><<<dim3(g.blocks, g.q_parts + g.k_parts), THREADS, 0, st>>>(h);
         return hipGetLastError();
     });
 }
@@ -362,9 +378,8 @@ hipError_t launch_headnorm_fwd(const void *q, const void *k, const float *wq, co
 
 size_t headnorm_scratch_bytes(int64_t rows, int q_heads, int k_heads, int head_dim)
 {
-    dim3 grid;
-    grid_of(rows, q_heads + k_heads, &grid);
-    return align_up((size_t)grid.x * grid.y * 2 * head_dim * 4, 256);
+    const HeadGrid g = grid_of(rows, q_heads, k_heads);
+    return align_up((size_t)g.blocks * (g.q_parts + g.k_parts) * head_dim * 4, 256);
 }
 
 hipError_t launch_headnorm_bwd(const void *q, const void *k, const float *wq, const float *wk, const int32_t *pos, const float *freq, const void *dyq,
@@ -374,9 +389,8 @@ hipError_t launch_headnorm_bwd(const void *q, const void *k, const float *wq, co
         ? launch<bf16_t, true>(q, k, wq, wk, pos, freq, dyq, dyk, dq, dk, s.ld_yq, s.ld_yk, s.ld_dq, s.ld_dk, s, (float *)scratch, st)
         : launch<float, true>(q, k, wq, wk, pos, freq, dyq, dyk, dq, dk, s.ld_yq, s.ld_yk, s.ld_dq, s.ld_dk, s, (float *)scratch, st);
     if (e != hipSuccess || (!dwq && !dwk)) return e;
-    dim3 grid;
-    grid_of(s.rows, s.q_heads + s.k_heads, &grid);
-    headnorm_sum_kernel<<<(2 * s.head_dim + 15) / 16, 1024, 0, st>>>((const float *)scratch, dwq, dwk, s.head_dim, (int)(grid.x * grid.y));
+    const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads);
+    headnorm_sum_kernel<<<dim3((s.head_dim + 15) / 16, 2), 1024, 0, st>>>((const float *)scratch, dwq, dwk, s.head_dim, g.blocks * g.q_parts, g.blocks * g.k_parts);
     return hipGetLastError();
 }
 
