@@ -11,34 +11,24 @@ template <> __device__ inline float seq_ld<bf16_t>(const bf16_t *p) { return bf1
 __device__ inline void seq_st(float *p, float v) { *p = v; }
 __device__ inline void seq_st(bf16_t *p, float v) { *p = f32_to_bf16(v); }
 
-// V neighbouring elements as they lie in memory.  Loaded and stored whole where they are aligned to their size and all there, one by
-// one otherwise; what is not there reads as zero.
+// V neighbouring elements as they lie in memory, loaded and stored in one access at their size's alignment.  What a lane has nothing to load
+// from it loads from some other place and leaves out later: a load under a condition of the lane's own would be waited for right
+// where the two ways meet, and nothing could be loaded ahead.
+template <int BYTES> struct Word;
+template <> struct Word<2> { typedef uint16_t type; };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Word<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack {
+    typedef typename Word<sizeof(T) * V>::type W;   // the access, as one value: a copy of the elements would be split up and stored in parts
     T e[V];
     __device__ void zero()
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) e[i] = 0;
     }
-    __device__ void load(const T *p, int n, bool whole)
-    {
-        if (whole && n >= V) {
-            *this = *reinterpret_cast<const Pack *>(p);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) e[i] = i < n ? p[i] : (T)0;
-    }
-    __device__ void store(T *p, int n, bool whole) const
-    {
-        if (whole && n >= V) {
-            *reinterpret_cast<Pack *>(p) = *this;
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) p[i] = e[i];
-    }
+    __device__ void load(const T *p) { *this = __builtin_bit_cast(Pack, *reinterpret_cast<const W *>(p)); }
+    __device__ void store(T *p) const { *reinterpret_cast<W *>(p) = __builtin_bit_cast(W, *this); }
     __device__ float get(int i) const { return seq_ld<T>(&e[i]); }
     __device__ void set(int i, float v) { seq_st(&e[i], v); }
 };

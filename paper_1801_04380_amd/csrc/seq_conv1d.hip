@@ -4,78 +4,94 @@
 // V neighbouring channels (16 bytes where the rows allow it) and walks down a run of rows with the taps' inputs in registers, so that an
 // input row is loaded once but for the width - 1 rows in front of the run.
 #include "seq.h"
+#include <initializer_list>
 
 namespace sn {
 namespace {
 
 constexpr int THREADS = 256;
 
-template <typename T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
-
 // The filters and biases of V channels, taps innermost in memory.
 template <typename T, int V, int W> struct Taps {
     float w[V][W], b[V];
-    __device__ void load(const T *wp, const float *bp, int c, int n)
+    __device__ void load(const T *wp, const float *bp, int c)
     {
-        Pack<T, V> raw[W];   // the V * W elements lie side by side
-        const bool whole = n >= V && reinterpret_cast<uintptr_t>(wp + (size_t)c * W) % (sizeof(T) * V) == 0;
-#pragma unroll
-        for (int j = 0; j < W; ++j) raw[j].load(wp + (size_t)c * W + j * V, n * W - j * V, whole);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            b[i] = bp && i < n ? bp[c + i] : 0.f;
+            b[i] = bp ? bp[c + i] : 0.f;
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[i][j] = raw[(i * W + j) / V].get((i * W + j) % V);
+            for (int j = 0; j < W; ++j) w[i][j] = seq_ld<T>(wp + (size_t)c * W + i * W + j);
         }
+    }
+    __device__ float p(int i, const Pack<T, V> *in) const   // of channel i from its W inputs
+    {
+        float v = b[i];
+#pragma unroll
+        for (int j = 0; j < W; ++j) v = fmaf(w[i][j], in[j].get(i), v);
+        return v;
     }
 };
 
+template <typename T, int V> __device__ inline void load_each(Pack<T, V> &v, const T *p)
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) v.e[i] = p[i];
+}
+template <typename T, int V> __device__ inline void store_each(const Pack<T, V> &v, T *p)
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = v.e[i];
+}
+
 // The input under a tap: row src of x where the sequence that begins at `begin` holds it, a row of the initial state in front of it.
 template <typename T, int V>
-__device__ inline Pack<T, V> tap_input(const T *x, int64_t ld, const T *state, int channels, int W, const SeqAt &at, int src, int c, int n, bool whole)
+__device__ inline Pack<T, V> tap_input(const T *x, int64_t ld, const T *state, int channels, int W, const SeqAt &at, int src, int c)
 {
     Pack<T, V> v;
-    if (src >= at.begin) v.load(x + (int64_t)src * ld + c, n, whole);
-    else if (state) v.load(state + ((int64_t)at.s * (W - 1) + (W - 1 + src - at.begin)) * channels + c, n, false);
+    if (src >= at.begin) v.load(x + (int64_t)src * ld + c);
+    else if (state) load_each(v, state + ((int64_t)at.s * (W - 1) + (W - 1 + src - at.begin)) * channels + c);
     else v.zero();
     return v;
 }
 
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, T *__restrict__ y,
-                                                             int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, bool whole_x,
-                                                             bool whole_y, const T *__restrict__ state_in, T *__restrict__ state_out)
+                                                             int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, const T *__restrict__ state_in, T *__restrict__ state_out)
 {
     constexpr int R = 8;   // rows at a time: their loads are all on their way before the first is used
-    const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V, n = channels - c;
-    if (n <= 0) return;
+    const int c = (blockIdx.x * THREADS + threadIdx.x) * V;
+    if (c >= channels) return;
     Taps<T, V, W> taps;
-    taps.load(w, bias, c, n);
+    taps.load(w, bias, c);
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
     if (r0 < r1) {
         SeqAt at = seq_find(rows, r0);
-        Pack<T, V> in[W - 1 + R];   // the rows in front, if the last turn was a whole one, and this turn's
+        Pack<T, V> in[W - 1 + R], ahead[R];   // the rows in front, if the last turn was a whole one, and this turn's; the next turn's
+        const auto fetch = [&](int b) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) ahead[k].load(x + (int64_t)min(b + k, r1 - 1) * ld_x + c);
+        };
         bool have = false;
+        fetch(r0);
         for (int b = r0; b < r1; b += R) {
             seq_forward(rows, at, b);
+#pragma unroll
+            for (int k = 0; k < R; ++k) in[W - 1 + k] = ahead[k];
+            fetch(b + R);
             if (at.holds(b, rows) && b - (W - 1) >= at.begin && b + R <= min(at.end, r1) && !(state_out && b + R == at.end)) {
                 if (!have)
 #pragma unroll
-                    for (int j = 0; j < W - 1; ++j) in[j].load(x + (int64_t)(b - (W - 1) + j) * ld_x + c, n, whole_x);
+                    for (int j = 0; j < W - 1; ++j) in[j].load(x + (int64_t)(b - (W - 1) + j) * ld_x + c);
                 have = true;
-#pragma unroll
-                for (int k = 0; k < R; ++k) in[W - 1 + k].load(x + (int64_t)(b + k) * ld_x + c, n, whole_x);
 #pragma unroll
                 for (int k = 0; k < R; ++k) {
                     Pack<T, V> out;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        float p = taps.b[i];
-#pragma unroll
-                        for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[k + j].get(i), p);
+                        const float p = taps.p(i, &in[k]);
                         out.set(i, silu ? p * sigmoid(p) : p);
                     }
-                    out.store(y + (int64_t)(b + k) * ld_y + c, n, whole_y);
+                    out.store(y + (int64_t)(b + k) * ld_y + c);
                 }
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j) in[j] = in[R + j];
@@ -88,18 +104,16 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
                 if (!at.holds(t, rows)) continue;
                 Pack<T, V> tap[W], out;
 #pragma unroll
-                for (int j = 0; j < W; ++j) tap[j] = tap_input<T, V>(x, ld_x, state_in, channels, W, at, t - (W - 1) + j, c, n, whole_x);
+                for (int j = 0; j < W; ++j) tap[j] = tap_input<T, V>(x, ld_x, state_in, channels, W, at, t - (W - 1) + j, c);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    float p = taps.b[i];
-#pragma unroll
-                    for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], tap[j].get(i), p);
+                    const float p = taps.p(i, tap);
                     out.set(i, silu ? p * sigmoid(p) : p);
                 }
-                out.store(y + (int64_t)t * ld_y + c, n, whole_y);
+                out.store(y + (int64_t)t * ld_y + c);
                 if (state_out && t == at.end - 1)
 #pragma unroll
-                    for (int j = 1; j < W; ++j) tap[j].store(state_out + ((int64_t)at.s * (W - 1) + j - 1) * channels + c, n, false);
+                    for (int j = 1; j < W; ++j) store_each(tap[j], state_out + ((int64_t)at.s * (W - 1) + j - 1) * channels + c);
             }
         }
     }
@@ -108,7 +122,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
         for (int s = 0; s < rows.seqs; ++s) {
             if (rows.off && rows.off[s] != rows.off[s + 1]) continue;
             for (int j = 0; j < W - 1; ++j)
-                for (int i = 0; i < min(n, V); ++i) {
+                for (int i = 0; i < V; ++i) {
                     const int64_t k = ((int64_t)s * (W - 1) + j) * channels + c + i;
                     state_out[k] = state_in ? state_in[k] : (T)0;
                 }
@@ -122,34 +136,6 @@ __device__ inline float silu_slope(float p)
     return s * (1.f + p * (1.f - s));
 }
 
-// p of row t, and with it dp.  A row that no sequence holds has none.
-template <typename T, int V, int W>
-__device__ inline void gradient_of_p(const T *x, const T *dy, const T *state, int channels, int silu, int64_t ld_x, int64_t ld_y, const SeqRows &rows, const SeqAt &at,
-                                     int t, int c, int n, bool whole_x, bool whole_y, const Taps<T, V, W> &taps, float (&dp)[V], Pack<T, V> (&in)[W])
-{
-    if (!at.holds(t, rows)) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) dp[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) in[j].zero();
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < W; ++j) in[j] = tap_input<T, V>(x, ld_x, state, channels, W, at, t - (W - 1) + j, c, n, whole_x);
-    Pack<T, V> g;
-    g.load(dy + (int64_t)t * ld_y + c, n, whole_y);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        dp[i] = g.get(i);
-        if (silu) {
-            float p = taps.b[i];
-#pragma unroll
-            for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[j].get(i), p);
-            dp[i] *= silu_slope(p);
-        }
-    }
-}
-
 // part[slice][W + 1][channels]: the slice's sums for dw, then for dbias.
 // A thread walks down the rows r0 .. r1 - 1 of its slice, R at a time.  A turn at b reads x and dy of the rows b + W - 1 .. b + R + W - 2,
 // makes their dp, and with the W - 1 rows in front, which it has, dx of rows b .. b + R - 1.  The first turn, at r0 - R, only fills what the next
@@ -157,14 +143,14 @@ __device__ inline void gradient_of_p(const T *x, const T *dy, const T *state, in
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, const T *__restrict__ dy,
                                                              T *__restrict__ dx, float *__restrict__ part, int channels, int silu, int64_t ld_x, int64_t ld_y,
-                                                             int64_t ld_dx, SeqRows rows, int run, bool whole_x, bool whole_y, bool whole_dx,
-                                                             const T *__restrict__ state_in, const T *__restrict__ dstate_out)
+                                                             int64_t ld_dx, SeqRows rows, int run, const T *__restrict__ state_in,
+                                                             const T *__restrict__ dstate_out)
 {
     constexpr int R = W <= 5 ? 8 : 16, H = W - 1;
-    const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V, n = channels - c;
-    if (n <= 0) return;
+    const int c = (blockIdx.x * THREADS + threadIdx.x) * V;
+    if (c >= channels) return;
     Taps<T, V, W> taps;
-    taps.load(w, bias, c, n);
+    taps.load(w, bias, c);
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
     float dw[V][W] = {}, db[V] = {};
     if (r0 < r1) {
@@ -174,10 +160,9 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
             Pack<T, V> xs[R], gs[R];
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                const int t = b + H + k;
-                const int m = t >= 0 && t < rows.rows ? n : 0;
-                xs[k].load(x + (int64_t)t * ld_x + c, m, whole_x);
-                gs[k].load(dy + (int64_t)t * ld_y + c, m, whole_y);
+                const int t = min(max(b + H + k, 0), rows.rows - 1);
+                xs[k].load(x + (int64_t)t * ld_x + c);
+                gs[k].load(dy + (int64_t)t * ld_y + c);
             }
             if (b >= r0) seq_forward(rows, trail, b);
             const bool plain = b >= r0 && b + H + R <= min(trail.end, r1) && trail.holds(b, rows);
@@ -211,7 +196,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
                         for (int j = 0; j < W; ++j) g = fmaf(taps.w[i][H - j], dp[k + j][i], g);
                         out.set(i, g);
                     }
-                    out.store(dx + (int64_t)(b + k) * ld_dx + c, n, whole_dx);
+                    out.store(dx + (int64_t)(b + k) * ld_dx + c);
                 }
             } else {
                 // the slice's or a sequence's first or last rows are among these
@@ -228,7 +213,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
                         for (int j = 0; j < W; ++j) {
                             const int src = t - H + j;
                             tap[j] = src >= lead.begin ? in[k + j][i] : 0.f;
-                            if (there && src < lead.begin && state_in && i < n)
+                            if (there && src < lead.begin && state_in)
                                 tap[j] = seq_ld<T>(state_in + ((int64_t)lead.s * H + H + src - lead.begin) * channels + c + i);
                             p = fmaf(taps.w[i][j], tap[j], p);
                         }
@@ -254,10 +239,10 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
 #pragma unroll
                         for (int j = 0; j < W; ++j)
                             if (t + j < trail.end) g = fmaf(taps.w[i][H - j], dp[k + j][i], g);
-                        if (dstate_out && t >= trail.end - H && i < n) g += seq_ld<T>(dstate_out + ((int64_t)trail.s * H + t - (trail.end - H)) * channels + c + i);
+                        if (dstate_out && t >= trail.end - H) g += seq_ld<T>(dstate_out + ((int64_t)trail.s * H + t - (trail.end - H)) * channels + c + i);
                         out.set(i, g);
                     }
-                    out.store(dx + (int64_t)t * ld_dx + c, n, whole_dx);
+                    out.store(dx + (int64_t)t * ld_dx + c);
                 }
             }
 #pragma unroll
@@ -275,7 +260,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
         Pack<float, V> v;
 #pragma unroll
         for (int i = 0; i < V; ++i) v.e[i] = j < W ? dw[i][j < W ? j : 0] : db[i];
-        v.store(to + (size_t)j * channels, n, channels % V == 0);
+        v.store(to + (size_t)j * channels);
     }
 }
 
@@ -295,14 +280,18 @@ __global__ void __launch_bounds__(THREADS) conv1d_dstate_kernel(const T *__restr
     }
     const int len = max(at.end - at.begin, 0);
     Taps<T, 1, W> taps;
-    taps.load(w, bias, c, 1);
+    taps.load(w, bias, c);
     float dp[W];  // of the sequence's first rows
 #pragma unroll
     for (int e = 0; e < W - 1; ++e) {
-        float one[1] = {0.f};
+        dp[e] = 0.f;
+        if (e >= len) continue;
+        const int t = at.begin + e;
         Pack<T, 1> in[W];
-        if (e < len) gradient_of_p<T, 1, W>(x, dy, state_in, channels, silu, ld_x, ld_y, rows, at, at.begin + e, c, 1, true, true, taps, one, in);
-        dp[e] = one[0];
+#pragma unroll
+        for (int j = 0; j < W; ++j) in[j] = tap_input<T, 1>(x, ld_x, state_in, channels, W, at, t - (W - 1) + j, c);
+        dp[e] = seq_ld<T>(dy + (int64_t)t * ld_y + c);
+        if (silu) dp[e] *= silu_slope(taps.p(0, in));
     }
 #pragma unroll
     for (int i = 0; i < W - 1; ++i) {   // the state's row i stands W - 1 - i rows in front of the sequence
@@ -337,28 +326,26 @@ __global__ void __launch_bounds__(THREADS) conv1d_sum_kernel(const float *__rest
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(THREADS) conv1d_step_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, T *__restrict__ y,
                                                               const T *state, T *state_out, const int32_t *__restrict__ slots, int num_slots, int channels,
-                                                              int silu, int64_t ld_x, int64_t ld_y, bool whole_x, bool whole_y, bool whole_s)
+                                                              int silu, int64_t ld_x, int64_t ld_y)
 {
-    const int c = (blockIdx.y * THREADS + threadIdx.x) * V, n = channels - c, row = blockIdx.x;
-    if (n <= 0) return;
+    const int c = (blockIdx.y * THREADS + threadIdx.x) * V, row = blockIdx.x;
+    if (c >= channels) return;
     const int slot = step_slot(slots, row, num_slots);
     if (slot < 0) return;
     Taps<T, V, W> taps;
-    taps.load(w, bias, c, n);
+    taps.load(w, bias, c);
     Pack<T, V> in[W], out;
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) in[j].load(state + ((int64_t)slot * (W - 1) + j) * channels + c, n, whole_s);
-    in[W - 1].load(x + (int64_t)row * ld_x + c, n, whole_x);
+    for (int j = 0; j < W - 1; ++j) in[j].load(state + ((int64_t)slot * (W - 1) + j) * channels + c);
+    in[W - 1].load(x + (int64_t)row * ld_x + c);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        float p = taps.b[i];
-#pragma unroll
-        for (int j = 0; j < W; ++j) p = fmaf(taps.w[i][j], in[j].get(i), p);
+        const float p = taps.p(i, in);
         out.set(i, silu ? p * sigmoid(p) : p);
     }
-    out.store(y + (int64_t)row * ld_y + c, n, whole_y);
+    out.store(y + (int64_t)row * ld_y + c);
 #pragma unroll
-    for (int j = 1; j < W; ++j) in[j].store(state_out + ((int64_t)slot * (W - 1) + j - 1) * channels + c, n, whole_s);
+    for (int j = 1; j < W; ++j) in[j].store(state_out + ((int64_t)slot * (W - 1) + j - 1) * channels + c);
 }
 
 // f(type, width) with both as types
@@ -393,38 +380,56 @@ int run_of(int64_t rows, int blocks, int least)
     return (int)(run < least ? least : run);
 }
 
+// The channels of a thread: MOST where every tensor's rows can be accessed so many at a time, else 2, else 1.
+template <int MOST, typename F> hipError_t by_vector(int most, F f)
+{
+    if (most >= MOST) return f(WidthIs<MOST>());
+    if (MOST > 2 && most >= 2) return f(WidthIs<2>());
+    return f(WidthIs<1>());
+}
+
+struct Rows2 {   // a tensor of rows
+    const void *p;
+    int64_t ld;
+};
+int vector_of(int channels, int esize, std::initializer_list<Rows2> tensors)
+{
+    int v = 16 / esize;
+    for (const Rows2 &t : tensors)
+        while (v > 1 && !(rows_aligned(t.p, t.ld, esize, v) && channels % v == 0)) v /= 2;
+    return v;
+}
+
 template <typename T> hipError_t fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off, const void *state_in,
                                      void *state_out, hipStream_t st)
 {
-    constexpr int V = vec_of<T>();
     return by_width(s.width, [&](auto W) {
-        const int blocks = div_up(s.channels, V * THREADS), run = run_of(s.rows, blocks, 32);
-        conv1d_fwd_kernel<T, V, W.value><<<dim3(blocks, s.rows ? div_up(s.rows, run) : 1), THREADS, 0, st>>>(
-            (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows_of(s, off), run, rows_aligned(x, s.ld_x, sizeof(T), V),
-            rows_aligned(y, s.ld_y, sizeof(T), V), (const T *)state_in, (T *)state_out);
-        return hipGetLastError();
+        return by_vector<16 / sizeof(T)>(vector_of(s.channels, sizeof(T), {{x, s.ld_x}, {y, s.ld_y}}), [&](auto V) {
+            const int blocks = div_up(s.channels, V.value * THREADS), run = run_of(s.rows, blocks, 32);
+            conv1d_fwd_kernel<T, V.value, W.value><<<dim3(blocks, s.rows ? div_up(s.rows, run) : 1), THREADS, 0, st>>>(
+                (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows_of(s, off), run, (const T *)state_in, (T *)state_out);
+            return hipGetLastError();
+        });
     });
 }
 
-constexpr int BWD_V = 4;   // channels of a thread: with 8 the windows of x and dp alone would take 176 registers
+constexpr int BWD_V = 4;   // channels of a thread at most: with 8 the windows of x and dp alone would take 176 registers
 
-int bwd_blocks(int channels) { return div_up(channels, BWD_V * THREADS); }
-
-// Rows of a slice: 64 at least, beside which the turn that fills the windows costs little.
-int bwd_run(int64_t rows, int channels) { return run_of(rows, bwd_blocks(channels), 64); }
+// Slices do not depend on how a call's tensors are aligned, so that the scratch does not either.
+int bwd_run(int64_t rows, int channels) { return run_of(rows, div_up(channels, BWD_V * THREADS), 64); }   // 64 rows: the turn that fills the windows costs little
 
 template <typename T> hipError_t bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
                                      const int32_t *off, const void *state_in, const void *dstate_out, void *dstate_in, void *scratch, hipStream_t st)
 {
-    constexpr int V = BWD_V;
     return by_width(s.width, [&](auto W) {
         const int run = bwd_run(s.rows, s.channels), slices = s.rows ? div_up(s.rows, run) : 1;
         const SeqRows rows = rows_of(s, off);
-        conv1d_bwd_kernel<T, V, W.value><<<dim3(div_up(s.channels, V * THREADS), slices), THREADS, 0, st>>>(
-            (const T *)x, (const T *)w, bias, (const T *)dy, (T *)dx, (float *)scratch, s.channels, s.silu, s.ld_x, s.ld_y, s.ld_dx, rows, run,
-            rows_aligned(x, s.ld_x, sizeof(T), V), rows_aligned(dy, s.ld_y, sizeof(T), V), rows_aligned(dx, s.ld_dx, sizeof(T), V), (const T *)state_in,
-            (const T *)dstate_out);
-        hipError_t e = hipGetLastError();
+        hipError_t e = by_vector<BWD_V>(vector_of(s.channels, sizeof(T), {{x, s.ld_x}, {dy, s.ld_y}, {dx, s.ld_dx}}), [&](auto V) {
+            conv1d_bwd_kernel<T, V.value, W.value><<<dim3(div_up(s.channels, V.value * THREADS), slices), THREADS, 0, st>>>(
+                (const T *)x, (const T *)w, bias, (const T *)dy, (T *)dx, (float *)scratch, s.channels, s.silu, s.ld_x, s.ld_y, s.ld_dx, rows, run,
+                (const T *)state_in, (const T *)dstate_out);
+            return hipGetLastError();
+        });
         if (e != hipSuccess) return e;
         conv1d_sum_kernel<<<dim3(div_up(s.channels, 16), s.width + 1), THREADS, 0, st>>>((const float *)scratch, dw, dbias, s.channels, s.width, slices);
         e = hipGetLastError();
@@ -438,13 +443,12 @@ template <typename T> hipError_t bwd(const void *x, const void *w, const float *
 template <typename T> hipError_t step(const void *x, const void *w, const float *bias, void *y, const void *state, void *state_out, const int32_t *slots, int num_slots,
                                       const sn_conv1d_shape &s, hipStream_t st)
 {
-    constexpr int V = vec_of<T>();
     return by_width(s.width, [&](auto W) {
-        const bool whole_s = rows_aligned(state, s.channels, sizeof(T), V) && rows_aligned(state_out, s.channels, sizeof(T), V);
-        conv1d_step_kernel<T, V, W.value><<<dim3((int)s.rows, div_up(s.channels, V * THREADS)), THREADS, 0, st>>>(
-            (const T *)x, (const T *)w, bias, (T *)y, (const T *)state, (T *)state_out, slots, num_slots, s.channels, s.silu, s.ld_x, s.ld_y,
-            rows_aligned(x, s.ld_x, sizeof(T), V), rows_aligned(y, s.ld_y, sizeof(T), V), whole_s);
-        return hipGetLastError();
+        return by_vector<16 / sizeof(T)>(vector_of(s.channels, sizeof(T), {{x, s.ld_x}, {y, s.ld_y}, {state, s.channels}, {state_out, s.channels}}), [&](auto V) {
+            conv1d_step_kernel<T, V.value, W.value><<<dim3((int)s.rows, div_up(s.channels, V.value * THREADS)), THREADS, 0, st>>>(
+                (const T *)x, (const T *)w, bias, (T *)y, (const T *)state, (T *)state_out, slots, num_slots, s.channels, s.silu, s.ld_x, s.ld_y);
+            return hipGetLastError();
+        });
     });
 }
 

@@ -32,31 +32,25 @@ struct HeadArgs {
 
 template <typename T, int E> struct Raw {   // a unit as it lies in memory
     Pack<T, E> lo, hi;
-    __device__ void zero()
+    __device__ void load(const T *head, int pa, int pb)
     {
-        lo.zero();
-        hi.zero();
-    }
-    __device__ void load(const T *head, int pa, int pb, int nb, bool pairs)
-    {
-        lo.load(head + pa, E, true);
-        if (pairs) hi.load(head + pa + E, E, true);
-        else if (nb) hi.load(head + pb, E, true);
-        else hi.zero();
+        lo.load(head + pa);
+        hi.load(head + pb);
     }
 };
 
 template <typename T, int E> struct Unit {
     float a[E], b[E];
     __device__ Unit() {}
-    __device__ Unit(const Raw<T, E> &r, bool pairs)
+    // has_a, has_b: whether the halves are there
+    __device__ Unit(const Raw<T, E> &r, bool pairs, bool has_a, bool has_b)
     {
 #pragma unroll
         for (int i = 0; i < E; ++i) {   // pairs: a, b alternate through the 2 E neighbours
             const float ea = 2 * i < E ? r.lo.get(2 * i < E ? 2 * i : 0) : r.hi.get(2 * i < E ? 0 : 2 * i - E);
             const float eb = 2 * i + 1 < E ? r.lo.get(2 * i + 1 < E ? 2 * i + 1 : 0) : r.hi.get(2 * i + 1 < E ? 0 : 2 * i + 1 - E);
-            a[i] = pairs ? ea : r.lo.get(i);
-            b[i] = pairs ? eb : r.hi.get(i);
+            a[i] = !has_a ? 0.f : pairs ? ea : r.lo.get(i);
+            b[i] = !has_b ? 0.f : pairs ? eb : r.hi.get(i);
         }
     }
     __device__ void store(T *head, int pa, int pb, int nb, bool pairs) const
@@ -68,16 +62,16 @@ template <typename T, int E> struct Unit {
                 if (2 * i < E) lo.set(2 * i < E ? 2 * i : 0, a[i]); else hi.set(2 * i < E ? 0 : 2 * i - E, a[i]);
                 if (2 * i + 1 < E) lo.set(2 * i + 1 < E ? 2 * i + 1 : 0, b[i]); else hi.set(2 * i + 1 < E ? 0 : 2 * i + 1 - E, b[i]);
             }
-            lo.store(head + pa, E, true);
-            hi.store(head + pa + E, E, true);
+            lo.store(head + pa);
+            hi.store(head + pa + E);
         } else {
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 lo.set(i, a[i]);
                 hi.set(i, b[i]);
             }
-            lo.store(head + pa, E, true);
-            if (nb) hi.store(head + pb, E, true);
+            lo.store(head + pa);
+            if (nb) hi.store(head + pb);
         }
     }
 };
@@ -158,19 +152,16 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
     const auto fetch = [&](int row, int head) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
-            const Place<E> p(u * LPH + l, h);
-            if (row < h.rows && head < h1 && p.there) {
-                rx[u].load((const T *)s.x + (int64_t)row * s.ld_x + (int64_t)head * h.head_dim, p.pa, p.pb, p.nb, p.pairs);
-                if (BWD) rg[u].load((const T *)s.g + (int64_t)row * s.ld_g + (int64_t)head * h.head_dim, p.pa, p.pb, p.nb, p.pairs);
-            } else {
-                rx[u].zero();
-                if (BWD) rg[u].zero();
-            }
+            const Place<E> p(u * LPH + l, h);   // without a condition, see Pack: from the last row, the last head, its first elements
+            const int pa = p.there ? p.pa : 0, pb = !p.there ? 0 : p.pairs ? p.pa + E : p.nb ? p.pb : 0;
+            const int64_t t = min(row, h.rows - 1), at = (int64_t)min(head, h1 - 1) * h.head_dim;
+            rx[u].load((const T *)s.x + t * s.ld_x + at, pa, pb);
+            if (BWD) rg[u].load((const T *)s.g + t * s.ld_g + at, pa, pb);
         }
     };
     int row = blockIdx.x * WAVES + wave;
-    fetch(row, h0 + group);
-    for (; row < h.rows; row += stride) {
+    if (h0 < h1 && h.rows) fetch(row, h0 + group);
+    for (; row < h.rows && h0 < h1; row += stride) {
         const int pos = h.positions ? h.positions[row] : row;
         for (int i = lane; i < h.rot_dim / 2; i += 64) {
             float c, sn;
@@ -200,8 +191,8 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 const Place<E> p(u * LPH + l, h);
-                v[u] = Unit<T, E>(rx[u], p.pairs);
-                if (BWD) d[u] = Unit<T, E>(rg[u], p.pairs);
+                v[u] = Unit<T, E>(rx[u], p.pairs, p.there, p.there && p.nb);
+                if (BWD) d[u] = Unit<T, E>(rg[u], p.pairs, here && p.there, here && p.there && p.nb);
 #pragma unroll
                 for (int i = 0; i < E; ++i) sum = fmaf(v[u].a[i], v[u].a[i], fmaf(v[u].b[i], v[u].b[i], sum));
             }

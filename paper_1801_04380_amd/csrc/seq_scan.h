@@ -170,24 +170,33 @@ template <int NL> struct ScanLane {
     }
 };
 
-// VE neighbouring channels of a row, as they lie in memory.
+// VE neighbouring channels of a row, as they lie in memory: of the nch channels from `base` on those from co on.  whole: in pieces (then a
+// thread's channels are all there or none is); otherwise one by one.
 template <typename T, int NL> struct Staged {
-    static constexpr int P = ScanGeo<NL>::template piece<T>(), PN = ScanGeo<NL>::VE / P;
+    static constexpr int VE = ScanGeo<NL>::VE, P = ScanGeo<NL>::template piece<T>(), PN = VE / P;
     Pack<T, P> p[PN];
-    __device__ void load(const void *base, int64_t at, int n, bool whole)
+    __device__ void load(const T *base, int co, int nch, bool whole)
     {
+        if (whole) {
+            const T *from = base + (co < nch ? co : 0);
 #pragma unroll
-        for (int i = 0; i < PN; ++i) p[i].load((const T *)base + at + i * P, n - i * P, whole);
+            for (int i = 0; i < PN; ++i) p[i].load(from + i * P);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VE; ++i) p[i / P].e[i % P] = base[min(co + i, nch - 1)];
+        }
     }
-    __device__ void store(void *base, int64_t at, int n, bool whole) const
+    __device__ void store(T *base, int co, int nch, bool whole) const
     {
+        if (whole) {
+            if (co < nch)
 #pragma unroll
-        for (int i = 0; i < PN; ++i) p[i].store((T *)base + at + i * P, n - i * P, whole);
-    }
-    __device__ void zero()
-    {
+                for (int i = 0; i < PN; ++i) p[i].store(base + co + i * P);
+        } else {
 #pragma unroll
-        for (int i = 0; i < PN; ++i) p[i].zero();
+            for (int i = 0; i < VE; ++i)
+                if (co + i < nch) base[co + i] = p[i / P].e[i % P];
+        }
     }
     __device__ float get(int i) const { return p[i / P].get(i % P); }
     __device__ void set(int i, float v) { p[i / P].set(i % P, v); }
@@ -195,22 +204,22 @@ template <typename T, int NL> struct Staged {
 
 // A row's B or C of one group: NP values, a thread's share of a tile.
 template <typename T, int NL> struct StagedBC {
-    static constexpr int COUNT = TS * ScanGeo<NL>::NP, PER = (COUNT + 255) / 256;
+    static constexpr int NP = ScanGeo<NL>::NP, COUNT = TS * NP, PER = (COUNT + 255) / 256;
     T v[PER];
-    __device__ void load(const void *base, int64_t ld, const Piece &p, int64_t column, int N)
-    {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int k = i * 256 + threadIdx.x, row = k / ScanGeo<NL>::NP, n = k % ScanGeo<NL>::NP;
-            v[i] = k < COUNT && n < N && p.holds(p.t0 + row) ? ((const T *)base)[(int64_t)(p.t0 + row) * ld + column + n] : (T)0;
-        }
-    }
-    __device__ void put(float *lds) const
+    __device__ void load(const T *column, int64_t ld, int t0, int rows, int N)
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int k = i * 256 + threadIdx.x;
-            if (k < COUNT) lds[k] = seq_ld<T>(&v[i]);
+            v[i] = column[(int64_t)min(t0 + k / NP % TS, rows - 1) * ld + min(k % NP, N - 1)];
+        }
+    }
+    __device__ void put(float *lds, const Piece &p, int N) const
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = i * 256 + threadIdx.x;
+            if (k < COUNT) lds[k] = k % NP < N && p.holds(p.t0 + k / NP) ? seq_ld<T>(&v[i]) : 0.f;
         }
     }
 };

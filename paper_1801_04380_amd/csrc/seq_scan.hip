@@ -50,13 +50,12 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
         Staged<T, NL> u, dt, z;
         StagedBC<T, NL> B, C;
         const auto fetch = [&]() {
-            const int64_t t = next.t0 + row;
-            const int n = next.holds((int)t) ? nco : 0;
-            u.load(a.u, t * a.ld_u + c0 + co, n, a.whole_u);
-            dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
-            if (OUT && a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
-            B.load(a.B, a.ld_b, next, (int64_t)group * a.N, a.N);
-            if (OUT) C.load(a.C, a.ld_c, next, (int64_t)group * a.N, a.N);
+            const int64_t t = min(next.t0 + row, a.rows.rows - 1);
+            u.load((const T *)a.u + t * a.ld_u + c0, co, nch, a.whole_u);
+            dt.load((const T *)a.dt + t * a.ld_dt + c0, co, nch, a.whole_dt);
+            if (OUT && a.z) z.load((const T *)a.z + t * a.ld_z + c0, co, nch, a.whole_z);
+            B.load((const T *)a.B + group * a.N, a.ld_b, next.t0, a.rows.rows, a.N);
+            if (OUT) C.load((const T *)a.C + group * a.N, a.ld_c, next.t0, a.rows.rows, a.N);
         };
         if (next.any) fetch();
         while (next.any) {
@@ -65,15 +64,16 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
             float uu[VE], gate[VE];
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                const float raw = dt.get(i) + bias[i], delta = in && i < nco ? (a.softplus ? softplus(raw) : raw) : 0.f;
-                uu[i] = u.get(i);
+                const bool here = in && i < nco;
+                const float raw = dt.get(i) + bias[i], delta = here ? (a.softplus ? softplus(raw) : raw) : 0.f;
+                uu[i] = here ? u.get(i) : 0.f;
                 s_delta[row][co + i] = delta;
                 s_x[row][co + i] = delta * uu[i];
                 gate[i] = 1.f;
                 if (OUT && a.z) gate[i] = z.get(i) * sigmoid(z.get(i));
             }
-            B.put(s_B);
-            if (OUT) C.put(s_C);
+            B.put(s_B, now, a.N);
+            if (OUT) C.put(s_C, now, a.N);
             __syncthreads();
             next = piece_from(a.rows, at, now.p1, r0, r1);
             if (next.any) fetch();
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
                 Staged<T, NL> y;
 #pragma unroll
                 for (int i = 0; i < VE; ++i) y.set(i, fmaf(skip[i], uu[i], s_y[row][co + i]) * gate[i]);
-                y.store(a.y, (int64_t)(now.t0 + row) * a.ld_y + c0 + co, nco, a.whole_y);
+                y.store((T *)a.y + (int64_t)(now.t0 + row) * a.ld_y + c0, co, nch, a.whole_y);
             }
         }
     }
@@ -258,11 +258,11 @@ ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off
     return a;
 }
 
-// Whether the rows of a tensor can be staged in whole pieces: its address, its stride and every block's first channel.
+// Whether the rows of a tensor can be staged in whole pieces: by its address, its stride and the channels of a group.
 int scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan)
 {
     const int e = s.dtype == SN_BF16 ? 2 : 4, ve = plan.CB / 16, piece = ve * e > 16 ? 16 / e : ve;
-    return rows_aligned(p, ld, e, piece) && (s.groups == 1 || s.channels / s.groups % piece == 0);
+    return rows_aligned(p, ld, e, piece) && s.channels / s.groups % ve == 0;
 }
 
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws)

@@ -43,12 +43,11 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     Staged<T, NL> dt, z, dy;
     StagedBC<T, NL> C;
     const auto fetch = [&]() {
-        const int64_t t = next.t0 + row;
-        const int n = next.holds((int)t) ? nco : 0;
-        dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
-        dy.load(a.dy, t * a.ld_y + c0 + co, n, a.whole_y);
-        if (a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
-        C.load(a.C, a.ld_c, next, (int64_t)group * a.N, a.N);
+        const int64_t t = min(next.t0 + row, a.rows.rows - 1);
+        dt.load((const T *)a.dt + t * a.ld_dt + c0, co, nch, a.whole_dt);
+        dy.load((const T *)a.dy + t * a.ld_y + c0, co, nch, a.whole_y);
+        if (a.z) z.load((const T *)a.z + t * a.ld_z + c0, co, nch, a.whole_z);
+        C.load((const T *)a.C + group * a.N, a.ld_c, next.t0, a.rows.rows, a.N);
     };
     if (next.any) fetch();
     while (next.any) {
@@ -56,11 +55,12 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
         const bool in = now.holds(now.t0 + row);
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
+            const bool here = in && i < nco;
             const float raw = dt.get(i) + bias[i];
-            s_delta[row][co + i] = in && i < nco ? (a.softplus ? softplus(raw) : raw) : 0.f;
-            s_g[row][co + i] = dy.get(i) * (a.z ? z.get(i) * sigmoid(z.get(i)) : 1.f);
+            s_delta[row][co + i] = here ? (a.softplus ? softplus(raw) : raw) : 0.f;
+            s_g[row][co + i] = here ? dy.get(i) * (a.z ? z.get(i) * sigmoid(z.get(i)) : 1.f) : 0.f;
         }
-        C.put(s_C);
+        C.put(s_C, now, a.N);
         __syncthreads();
         next = piece_before(a.rows, at, now.p0, r0);
         if (next.any) fetch();
@@ -130,14 +130,13 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
         Staged<T, NL> u, dt, z, dy;
         StagedBC<T, NL> B, C;
         const auto fetch = [&]() {
-            const int64_t t = next.t0 + row;
-            const int n = next.holds((int)t) ? nco : 0;
-            u.load(a.u, t * a.ld_u + c0 + co, n, a.whole_u);
-            dt.load(a.dt, t * a.ld_dt + c0 + co, n, a.whole_dt);
-            dy.load(a.dy, t * a.ld_y + c0 + co, n, a.whole_y);
-            if (a.z) z.load(a.z, t * a.ld_z + c0 + co, n, a.whole_z);
-            B.load(a.B, a.ld_b, next, (int64_t)group * a.N, a.N);
-            C.load(a.C, a.ld_c, next, (int64_t)group * a.N, a.N);
+            const int64_t t = min(next.t0 + row, a.rows.rows - 1);
+            u.load((const T *)a.u + t * a.ld_u + c0, co, nch, a.whole_u);
+            dt.load((const T *)a.dt + t * a.ld_dt + c0, co, nch, a.whole_dt);
+            dy.load((const T *)a.dy + t * a.ld_y + c0, co, nch, a.whole_y);
+            if (a.z) z.load((const T *)a.z + t * a.ld_z + c0, co, nch, a.whole_z);
+            B.load((const T *)a.B + group * a.N, a.ld_b, next.t0, a.rows.rows, a.N);
+            C.load((const T *)a.C + group * a.N, a.ld_c, next.t0, a.rows.rows, a.N);
         };
         if (next.any) fetch();
         while (next.any) {
@@ -146,13 +145,14 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
             Staged<T, NL> u0 = u, dt0 = dt, z0 = z, dy0 = dy;   // as loaded: what is made of them is in LDS, or made again
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                const float raw = dt.get(i) + bias[i], delta = in && i < nco ? (a.softplus ? softplus(raw) : raw) : 0.f;
+                const bool here = in && i < nco;
+                const float raw = dt.get(i) + bias[i], delta = here ? (a.softplus ? softplus(raw) : raw) : 0.f;
                 s_delta[row][co + i] = delta;
-                s_x[row][co + i] = delta * u.get(i);
-                s_g[row][co + i] = a.z ? dy.get(i) * (z.get(i) * sigmoid(z.get(i))) : dy.get(i);
+                s_x[row][co + i] = here ? delta * u.get(i) : 0.f;
+                s_g[row][co + i] = here ? (a.z ? dy.get(i) * (z.get(i) * sigmoid(z.get(i))) : dy.get(i)) : 0.f;
             }
-            B.put(s_B);
-            C.put(s_C);
+            B.put(s_B, now, a.N);
+            C.put(s_C, now, a.N);
             __syncthreads();
             float first[4];   // the state in front of the piece
             if (!now.start) lane.load_own(a.states, (int64_t)span * a.tiles_per_span + (now.t0 - span * a.span_rows) / TS, a, first);
@@ -283,17 +283,17 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                         dD[i] = fmaf(gy, uu, dD[i]);
                     }
                 }
-                o.store(a.du, t * a.ld_du + c0 + co, nco, a.whole_du);
+                o.store((T *)a.du + t * a.ld_du + c0, co, nch, a.whole_du);
 #pragma unroll
                 for (int i = 0; i < VE; ++i) o.set(i, dd[i]);
-                o.store(a.ddt, t * a.ld_ddt + c0 + co, nco, a.whole_ddt);
+                o.store((T *)a.ddt + t * a.ld_ddt + c0, co, nch, a.whole_ddt);
                 if (a.z) {
 #pragma unroll
                     for (int i = 0; i < VE; ++i) {
                         const float zz = z0.get(i), s = sigmoid(zz);
                         o.set(i, dy0.get(i) * fmaf(skip[i], u0.get(i), s_y[row][co + i]) * s * (1.f + zz * (1.f - s)));
                     }
-                    o.store(a.dz, t * a.ld_dz + c0 + co, nco, a.whole_dz);
+                    o.store((T *)a.dz + t * a.ld_dz + c0, co, nch, a.whole_dz);
                 }
             }
             for (int k = threadIdx.x; k < TS * 2 * NP; k += THREADS) {
