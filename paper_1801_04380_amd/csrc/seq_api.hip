@@ -78,6 +78,9 @@ sn_status check_scan_sizes(const sn_scan_shape *s)
     return check_rows(s->rows, s->seqs, s->ragged);
 }
 
+// The kernels keep a row's stride in 32 bits, the place in a tile of 32 rows in as many.
+bool wide(int64_t ld) { return ld > (1 << 24); }
+
 sn_status check_scan(const sn_scan_shape *s, const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias,
                      const void *y)
 {
@@ -91,6 +94,7 @@ sn_status check_scan(const sn_scan_shape *s, const void *u, const void *dt, cons
     if (!stride(s->ld_u, s->channels, s->rows) || !stride(s->ld_dt, s->channels, s->rows) || !stride(s->ld_b, gn, s->rows) || !stride(s->ld_c, gn, s->rows) ||
         !stride(s->ld_y, s->channels, s->rows) || (z && !stride(s->ld_z, s->channels, s->rows)))
         return SN_ERR_BAD_ARG;
+    if (s->rows > 1 && (wide(s->ld_u) || wide(s->ld_dt) || wide(s->ld_b) || wide(s->ld_c) || wide(s->ld_y) || (z && wide(s->ld_z)))) return SN_ERR_UNSUPPORTED;
     return SN_OK;
 }
 
@@ -222,6 +226,7 @@ sn_status sn_scan_bwd(const void *u, const void *dt, const float *A, const void 
     if (!stride(shape->ld_du, shape->channels, rows) || !stride(shape->ld_ddt, shape->channels, rows) || !stride(shape->ld_db, gn, rows) || !stride(shape->ld_dc, gn, rows) ||
         (dz && !stride(shape->ld_dz, shape->channels, rows)))
         return SN_ERR_BAD_ARG;
+    if (rows > 1 && (wide(shape->ld_du) || wide(shape->ld_ddt) || wide(shape->ld_db) || wide(shape->ld_dc) || (dz && wide(shape->ld_dz)))) return SN_ERR_UNSUPPORTED;
     const void *in[] = {u, dt, z, dy, B, C}, *out[] = {du, ddt, dz, dB, dC};
     for (const void *o : out) {
         for (const void *i : in)

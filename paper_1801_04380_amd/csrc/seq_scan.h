@@ -12,7 +12,7 @@
 
 namespace sn {
 
-constexpr int TS = 16;   // rows of a tile, and between two kept states
+constexpr int TS = 16;   // rows between two kept states; of a tile in the backward pass
 
 template <int NL> struct ScanGeo {
     static constexpr int CW = 64 / NL, CB = 4 * CW, NP = 4 * NL;
@@ -24,28 +24,28 @@ struct ScanArgs {
     const void *u, *dt, *B, *C, *z, *dy;
     const float *A, *D, *bias;
     void *y, *du, *ddt, *dB, *dC, *dz;
-    int64_t ld_u, ld_dt, ld_b, ld_c, ld_z, ld_y, ld_du, ld_ddt, ld_db, ld_dc, ld_dz;
+    uint32_t ld_u, ld_dt, ld_b, ld_c, ld_z, ld_y, ld_du, ld_ddt, ld_db, ld_dc, ld_dz;   // row strides in bytes, 2^26 at most
     const float *h0, *dhT;
     float *hT, *dh0, *states;
     SeqRows rows;
     int channels, N, per_group, blocks_per_group, softplus;
     int span_rows, chunk_rows, parts, spans, tiles_per_span;  // a span (a sequence, or all rows) in `parts` chunks
-    float *carry, *sum_delta;                                 // [chunk][channels][N], [chunk][channels]
+    float *carry, *sum_delta;                                 // [chunk][channels][NP], [chunk][channels]
     int *through;                                             // [chunk]: no sequence ends and begins in it
+    int NP;                                                   // the states of the library's own arrays: padded to four for each lane
     float *part_a, *part_d, *part_bias, *part_bc;             // sums of chunks; of channel blocks [block][row][2][NP]
-    int whole_u, whole_dt, whole_z, whole_y, whole_du, whole_ddt, whole_dz;
+    int gate;   // z is there; if not, z is u: loaded and left out
 };
 
-// The rows p0 .. p1 - 1 that one turn of a kernel's loop works on: those of one sequence in the tile of rows t0 .. t0 + TS - 1.  The tile's other
+// The rows p0 .. p1 - 1 that one turn of a kernel's loop works on: those of one sequence in the tile of rows t0 .. t0 + ROWS - 1.  The tile's other
 // rows are staged as zeros: delta = 0 leaves the states, and the gradient on its way through them, as they are.
 struct Piece {
     int t0, p0, p1, seq;
     bool any, start, end;   // whether there is one; it begins, ends its sequence
     __device__ bool holds(int row) const { return any && row >= p0 && row < p1; }
-    __device__ bool full() const { return p1 - p0 == TS; }
 };
 // The first piece at or behind row `from` of the chunk r0 .. r1 - 1.  `at`: the place of an earlier row.
-__device__ inline Piece piece_from(const SeqRows &r, SeqAt &at, int from, int r0, int r1)
+template <int ROWS> __device__ inline Piece piece_from(const SeqRows &r, SeqAt &at, int from, int r0, int r1)
 {
     Piece p = {};
     if (at.s < 0 && from < r1) at = seq_clamped(r, 0);
@@ -56,14 +56,14 @@ __device__ inline Piece piece_from(const SeqRows &r, SeqAt &at, int from, int r0
     p.any = true;
     p.seq = at.s;
     p.p0 = from;
-    p.t0 = r0 + (from - r0) / TS * TS;
-    p.p1 = min(min(p.t0 + TS, at.end), r1);
+    p.t0 = r0 + (from - r0) / ROWS * ROWS;
+    p.p1 = min(min(p.t0 + ROWS, at.end), r1);
     p.start = from == at.begin;
     p.end = p.p1 == at.end;
     return p;
 }
 // The last piece in front of row `to`.  `at`: the place of a later row.
-__device__ inline Piece piece_before(const SeqRows &r, SeqAt &at, int to, int r0)
+template <int ROWS> __device__ inline Piece piece_before(const SeqRows &r, SeqAt &at, int to, int r0)
 {
     Piece p = {};
     if (at.s >= r.seqs && to > r0) at = seq_clamped(r, r.seqs - 1);
@@ -77,7 +77,7 @@ __device__ inline Piece piece_before(const SeqRows &r, SeqAt &at, int to, int r0
     p.any = true;
     p.seq = at.s;
     p.p1 = to;
-    p.t0 = r0 + (to - 1 - r0) / TS * TS;
+    p.t0 = r0 + (to - 1 - r0) / ROWS * ROWS;
     p.p0 = max(p.t0, at.begin);
     p.start = p.p0 == at.begin;
     p.end = to == at.end;
@@ -141,25 +141,30 @@ template <int NL> struct ScanLane {
 #pragma unroll
         for (int i = 0; i < 4; ++i) A2[i] = there && n0 + i < a.N ? a.A[(int64_t)channel * a.N + n0 + i] * 1.44269504088896340736f : 0.f;
     }
-    // the same for the library's own arrays, whose rows of states are aligned where N is a multiple of 4
-    __device__ void load_own(const float *p, int64_t k, const ScanArgs &a, float (&v)[4]) const
+    // Four states of one of the library's own arrays, [..][channels][NP]: padded, so that they are one access.  In two steps: a load without a
+    // condition, and the choice of what is there.
+    __device__ float4 fetch_own(const float *p, int64_t k, const ScanArgs &a) const
     {
-        if (a.N % 4) return load(p, k, a, v);
-        float4 q = {0.f, 0.f, 0.f, 0.f};
-        if (there && n0 < a.N) q = *reinterpret_cast<const float4 *>(p + (k * a.channels + channel) * a.N + n0);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        return *reinterpret_cast<const float4 *>(p + (k * a.channels + (there ? channel : channel - c)) * ScanGeo<NL>::NP + n0);
     }
+    __device__ void take(const float4 &q, const ScanArgs &a, float (&v)[4]) const
+    {
+        v[0] = there && n0 < a.N ? q.x : 0.f;
+        v[1] = there && n0 + 1 < a.N ? q.y : 0.f;
+        v[2] = there && n0 + 2 < a.N ? q.z : 0.f;
+        v[3] = there && n0 + 3 < a.N ? q.w : 0.f;
+    }
+    __device__ void load_own(const float *p, int64_t k, const ScanArgs &a, float (&v)[4]) const { take(fetch_own(p, k, a), a, v); }
     __device__ void store_own(float *p, int64_t k, const ScanArgs &a, const float (&v)[4]) const
     {
-        if (a.N % 4) return store(p, k, a, v);
-        if (there && n0 < a.N) *reinterpret_cast<float4 *>(p + (k * a.channels + channel) * a.N + n0) = make_float4(v[0], v[1], v[2], v[3]);
+        if (there) *reinterpret_cast<float4 *>(p + (k * a.channels + channel) * ScanGeo<NL>::NP + n0) = make_float4(v[0], v[1], v[2], v[3]);
     }
-    // four states of array p, [..][channels][N], at index k of its first dimension
+    // Four states of array p, [..][channels][N], at index k of its first dimension.  The choice of what is there waits for them, so that nothing
+    // has to where the ways from a call under a condition meet.
     __device__ void load(const float *p, int64_t k, const ScanArgs &a, float (&v)[4]) const
     {
-        const float *q = p + (k * a.channels + channel) * a.N + n0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = there && n0 + i < a.N ? q[i] : 0.f;
+        const float *q = p + (k * a.channels + (there ? channel : channel - c)) * a.N;
+        take(make_float4(q[min(n0, a.N - 1)], q[min(n0 + 1, a.N - 1)], q[min(n0 + 2, a.N - 1)], q[min(n0 + 3, a.N - 1)]), a, v);
     }
     __device__ void store(float *p, int64_t k, const ScanArgs &a, const float (&v)[4]) const
     {
@@ -170,56 +175,53 @@ template <int NL> struct ScanLane {
     }
 };
 
-// VE neighbouring channels of a row, as they lie in memory: of the nch channels from `base` on those from co on.  whole: in pieces (then a
-// thread's channels are all there or none is); otherwise one by one.
-template <typename T, int NL> struct Staged {
-    static constexpr int VE = ScanGeo<NL>::VE, P = ScanGeo<NL>::template piece<T>(), PN = VE / P;
+// Choices as one instruction and no branch, which would cut the code around it into pieces that nothing is moved across: v or zero; a where the
+// mask is all ones, b where it is zero.
+__device__ inline float keep_if(bool here, float v) { return __uint_as_float(__float_as_uint(v) & (here ? ~0u : 0u)); }
+__device__ inline float pick(uint32_t mask, float a, float b) { return __uint_as_float((__float_as_uint(a) & mask) | (__float_as_uint(b) & ~mask)); }
+
+// VE neighbouring channels of a row, as they lie in memory: of the nch channels that a row of the tile at `tile` begins with (the place of its
+// first row, the same for all lanes: the lane's part of an address is 32 bits) those from co on.  WHOLE: in pieces (then a thread's channels
+// are all there or none is); otherwise one by one.
+template <typename T, int NL, bool WHOLE> struct Staged {
+    static constexpr int VE = ScanGeo<NL>::VE, P = WHOLE ? ScanGeo<NL>::template piece<T>() : 1, PN = VE / P;
     Pack<T, P> p[PN];
-    __device__ void load(const T *base, int co, int nch, bool whole)
+    __device__ void load(const char *tile, uint32_t ld, int row, int co, int nch)
     {
-        if (whole) {
-            const T *from = base + (co < nch ? co : 0);
 #pragma unroll
-            for (int i = 0; i < PN; ++i) p[i].load(from + i * P);
-        } else {
-#pragma unroll
-            for (int i = 0; i < VE; ++i) p[i / P].e[i % P] = base[min(co + i, nch - 1)];
+        for (int i = 0; i < PN; ++i) {
+            const int c = WHOLE ? (co < nch ? co + i * P : 0) : min(co + i, nch - 1);
+            p[i].load(reinterpret_cast<const T *>(tile + (uint32_t)(row * ld + c * (uint32_t)sizeof(T))));
         }
     }
-    __device__ void store(T *base, int co, int nch, bool whole) const
+    __device__ void store(char *tile, uint32_t ld, int row, int co, int nch) const
     {
-        if (whole) {
-            if (co < nch)
 #pragma unroll
-                for (int i = 0; i < PN; ++i) p[i].store(base + co + i * P);
-        } else {
-#pragma unroll
-            for (int i = 0; i < VE; ++i)
-                if (co + i < nch) base[co + i] = p[i / P].e[i % P];
-        }
+        for (int i = 0; i < PN; ++i)
+            if (co + i * P < nch) p[i].store(reinterpret_cast<T *>(tile + (uint32_t)(row * ld + (co + i * P) * (uint32_t)sizeof(T))));
     }
     __device__ float get(int i) const { return p[i / P].get(i % P); }
     __device__ void set(int i, float v) { p[i / P].set(i % P, v); }
 };
 
-// A row's B or C of one group: NP values, a thread's share of a tile.
-template <typename T, int NL> struct StagedBC {
-    static constexpr int NP = ScanGeo<NL>::NP, COUNT = TS * NP, PER = (COUNT + 255) / 256;
+// A row's B or C of one group: NP values, a thread's share of a tile, of which the first `rows` are in the tensor.
+template <typename T, int NL, int ROWS> struct StagedBC {
+    static constexpr int NP = ScanGeo<NL>::NP, COUNT = ROWS * NP, PER = (COUNT + 255) / 256;
     T v[PER];
-    __device__ void load(const T *column, int64_t ld, int t0, int rows, int N)
+    __device__ void load(const char *tile, uint32_t ld, int rows, int N)
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int k = i * 256 + threadIdx.x;
-            v[i] = column[(int64_t)min(t0 + k / NP % TS, rows - 1) * ld + min(k % NP, N - 1)];
+            v[i] = *reinterpret_cast<const T *>(tile + (uint32_t)(min(k / NP % ROWS, rows - 1) * ld + min(k % NP, N - 1) * (uint32_t)sizeof(T)));
         }
     }
-    __device__ void put(float *lds, const Piece &p, int N) const
+    __device__ void put(float *lds, int first, int last, int N) const   // rows first .. last - 1 of the tile, zeros around them
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int k = i * 256 + threadIdx.x;
-            if (k < COUNT) lds[k] = k % NP < N && p.holds(p.t0 + k / NP) ? seq_ld<T>(&v[i]) : 0.f;
+            const int k = i * 256 + threadIdx.x, r = k / NP;
+            if (k < COUNT) lds[k] = k % NP < N && r >= first && r < last ? seq_ld<T>(&v[i]) : 0.f;
         }
     }
 };
@@ -233,10 +235,11 @@ struct ScanPlan {
 ScanPlan scan_plan(const sn_scan_shape &s, int parts);
 int scan_parts_wanted(const sn_scan_shape &s, bool bwd);
 size_t scan_carry_bytes(const sn_scan_shape &s, const ScanPlan &p);
-ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off);
-int scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan);
+ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off, const void *u, const void *dt, const float *A, const void *B, const void *C,
+                   const float *D, const void *z, const float *bias);
+bool scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan);
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws);
-hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st);   // a.states from the inputs
+hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st);   // a.states from the inputs
 hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st);
 
 template <int V> struct ScanInt { static constexpr int value = V; };

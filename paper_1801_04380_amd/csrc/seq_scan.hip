@@ -8,6 +8,7 @@
 // final state from a zero one and its sum of delta (the product of its decays is exp(A * sum)), scan_carry_kernel joins them, and the
 // second pass starts each chunk from its state.
 #include "seq_scan.h"
+#include <cstdlib>
 
 namespace sn {
 namespace {
@@ -16,15 +17,17 @@ constexpr int THREADS = 256;
 
 // MODE 0: y (and, if asked for, the states of tiles and the final states); 1: the chunk's final state from zero and the sum of delta;
 // 2: the states of tiles alone.
-template <typename T, int NL, int MODE>
+template <typename T, int NL, bool WHOLE, int MODE>
 __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
     constexpr int CB = G::CB, NP = G::NP, VE = G::VE;
     constexpr bool OUT = MODE == 0, LOCAL = MODE == 1;
-    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_y[OUT ? TS : 1][OUT ? CB : 1];
-    __shared__ alignas(16) float s_B[TS * NP];
-    __shared__ alignas(16) float s_C[OUT ? TS * NP : 4];
+    // Rows staged at a time.  The loads of the next ones are on their way while these are worked on; 16 rows are too little work to cover them.
+    constexpr int ROWS = 32, RP = ROWS / 16;
+    __shared__ float s_delta[ROWS][CB], s_x[ROWS][CB], s_y[OUT ? ROWS : 1][OUT ? CB : 1];
+    __shared__ alignas(16) float s_B[ROWS * NP];
+    __shared__ alignas(16) float s_C[OUT ? ROWS * NP : 4];
 
     const int chunk = blockIdx.x, span = chunk / a.parts, part = chunk % a.parts;
     if (LOCAL && part == a.parts - 1) return;   // nothing comes after it
@@ -40,53 +43,73 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
         bias[i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
         skip[i] = OUT && a.D && i < nco ? a.D[c0 + co + i] : 0.f;
     }
+    const char *pu = (const char *)a.u + c0 * sizeof(T), *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T);
+    const char *pB = (const char *)a.B + group * a.N * sizeof(T), *pC = (const char *)a.C + group * a.N * sizeof(T);
+    char *py = (char *)a.y + c0 * sizeof(T);
+    const uint32_t is_softplus = a.softplus ? ~0u : 0u, is_gate = a.gate ? ~0u : 0u;
     float h[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
     bool crossed = false;
     if (!LOCAL && part > 0) lane.load_own(a.carry, chunk, a, h);
 
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, r0);
-        Piece next = piece_from(a.rows, at, r0, r0, r1);
-        Staged<T, NL> u, dt, z;
-        StagedBC<T, NL> B, C;
+        Piece next = piece_from<ROWS>(a.rows, at, r0, r0, r1);
+        Staged<T, NL, WHOLE> u[RP], dt[RP], z[RP];
+        StagedBC<T, NL, ROWS> B, C;
         const auto fetch = [&]() {
-            const int64_t t = min(next.t0 + row, a.rows.rows - 1);
-            u.load((const T *)a.u + t * a.ld_u + c0, co, nch, a.whole_u);
-            dt.load((const T *)a.dt + t * a.ld_dt + c0, co, nch, a.whole_dt);
-            if (OUT && a.z) z.load((const T *)a.z + t * a.ld_z + c0, co, nch, a.whole_z);
-            B.load((const T *)a.B + group * a.N, a.ld_b, next.t0, a.rows.rows, a.N);
-            if (OUT) C.load((const T *)a.C + group * a.N, a.ld_c, next.t0, a.rows.rows, a.N);
-        };
-        if (next.any) fetch();
-        while (next.any) {
-            const Piece now = next;
-            const bool in = now.holds(now.t0 + row);
-            float uu[VE], gate[VE];
+            const int64_t t0 = next.t0;
+            const int have = a.rows.rows - next.t0;   // rows of the tensors from there on
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                const bool here = in && i < nco;
-                const float raw = dt.get(i) + bias[i], delta = here ? (a.softplus ? softplus(raw) : raw) : 0.f;
-                uu[i] = here ? u.get(i) : 0.f;
-                s_delta[row][co + i] = delta;
-                s_x[row][co + i] = delta * uu[i];
-                gate[i] = 1.f;
-                if (OUT && a.z) gate[i] = z.get(i) * sigmoid(z.get(i));
+            for (int j = 0; j < RP; ++j) {
+                const int r = min(j * 16 + row, have - 1);
+                u[j].load(pu + t0 * a.ld_u, a.ld_u, r, co, nch);
+                dt[j].load(pdt + t0 * a.ld_dt, a.ld_dt, r, co, nch);
+                if (OUT) z[j].load(pz + t0 * a.ld_z, a.ld_z, r, co, nch);
             }
-            B.put(s_B, now, a.N);
-            if (OUT) C.put(s_C, now, a.N);
-            __syncthreads();
-            next = piece_from(a.rows, at, now.p1, r0, r1);
+            B.load(pB + t0 * a.ld_b, a.ld_b, have, a.N);
+            if (OUT) C.load(pC + t0 * a.ld_c, a.ld_c, have, a.N);
+        };
+        float uu[RP][VE], gate[RP][VE];
+        const auto stage = [&](const Piece &p) {
+            const int first = p.p0 - p.t0, last = p.p1 - p.t0;
+#pragma unroll
+            for (int j = 0; j < RP; ++j) {
+                const int r = j * 16 + row;
+                const bool in = r >= first && r < last;
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    const bool here = in && i < nco;
+                    const float raw = dt[j].get(i) + bias[i], delta = keep_if(here, pick(is_softplus, softplus(raw), raw));
+                    uu[j][i] = keep_if(here, u[j].get(i));
+                    s_delta[r][co + i] = delta;
+                    s_x[r][co + i] = delta * uu[j][i];
+                    if (OUT) gate[j][i] = pick(is_gate, z[j].get(i) * sigmoid(z[j].get(i)), 1.f);
+                }
+            }
+            B.put(s_B, first, last, a.N);
+            if (OUT) C.put(s_C, first, last, a.N);
+        };
+        Piece now = next;
+        if (now.any) {
+            fetch();
+            stage(now);
+            next = piece_from<ROWS>(a.rows, at, now.p1, r0, r1);
             if (next.any) fetch();
+        }
+        __syncthreads();
+        while (now.any) {
+            const auto keep = [&](int t) { lane.store_own(a.states, (int64_t)span * a.tiles_per_span + (now.t0 + t - span * a.span_rows) / TS, a, h); };
             if (now.start) {
                 crossed = true;
                 sum_delta = 0.f;
                 if (a.h0) lane.load(a.h0, now.seq, a, h);
                 else h[0] = h[1] = h[2] = h[3] = 0.f;
             } else if (!LOCAL && a.states && now.p0 == now.t0) {
-                lane.store_own(a.states, (int64_t)span * a.tiles_per_span + (now.t0 - span * a.span_rows) / TS, a, h);
+                keep(0);
             }
 
             const auto rows = [&](int tb) {   // NL rows, and the sums of their outputs
+                if (!LOCAL && a.states && tb && tb % TS == 0 && now.t0 + tb > now.p0) keep(tb);
                 float acc[NL];
 #pragma unroll
                 for (int k = 0; k < NL; ++k) {
@@ -107,20 +130,34 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
                 }
                 if (OUT) s_y[tb + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
             };
-            if (now.full()) {
+            if (now.p1 - now.p0 == ROWS) {
 #pragma unroll
-                for (int tb = 0; tb < TS; tb += NL) rows(tb);
+                for (int tb = 0; tb < ROWS; tb += NL) rows(tb);
             } else {
                 for (int tb = (now.p0 - now.t0) / NL * NL; tb < now.p1 - now.t0; tb += NL) rows(tb);
             }
             if (OUT && a.hT && now.end) lane.store(a.hT, now.seq, a, h);
             __syncthreads();
-            if (OUT && in) {
-                Staged<T, NL> y;
+            Staged<T, NL, WHOLE> y[RP];
+            if (OUT)
 #pragma unroll
-                for (int i = 0; i < VE; ++i) y.set(i, fmaf(skip[i], uu[i], s_y[row][co + i]) * gate[i]);
-                y.store((T *)a.y + (int64_t)(now.t0 + row) * a.ld_y + c0, co, nch, a.whole_y);
+                for (int j = 0; j < RP; ++j)
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) y[j].set(i, fmaf(skip[i], uu[j][i], s_y[j * 16 + row][co + i]) * gate[j][i]);
+            // The next rows are staged before anything is stored: whoever waits for the loads waits for what was stored since as well.
+            if (next.any) stage(next);
+            if (OUT)
+#pragma unroll
+                for (int j = 0; j < RP; ++j) {
+                    const int r = j * 16 + row;
+                    if (now.holds(now.t0 + r)) y[j].store(py + (int64_t)now.t0 * a.ld_y, a.ld_y, r, co, nch);
+                }
+            now = next;
+            if (now.any) {
+                next = piece_from<ROWS>(a.rows, at, now.p1, r0, r1);
+                if (next.any) fetch();
             }
+            __syncthreads();
         }
     }
     if (LOCAL) {
@@ -141,10 +178,10 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
 // reaches a chunk from the one behind it.
 __global__ void __launch_bounds__(THREADS) scan_carry_kernel(ScanArgs a, int reverse)
 {
-    const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.N;
+    const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.NP;
     if (i >= each) return;
-    const int channel = (int)(i / a.N);
-    const float A2 = a.A[i] * 1.44269504088896340736f;
+    const int channel = (int)(i / a.NP), n = (int)(i % a.NP);
+    const float A2 = n < a.N ? a.A[(int64_t)channel * a.N + n] * 1.44269504088896340736f : 0.f;
     float v = 0.f;
     for (int k = 0; k < a.parts; ++k) {
         const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - k : k);
@@ -171,11 +208,11 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     const int k = blockIdx.y * THREADS + threadIdx.x, c = k / NL, n0 = k % NL * 4;
     if (c >= a.channels) return;
     const int group = c / a.per_group;
-    const float u = seq_ld<T>((const T *)a.u + t * a.ld_u + c);
-    float raw = seq_ld<T>((const T *)a.dt + t * a.ld_dt + c);
+    const float u = seq_ld<T>((const T *)((const char *)a.u + t * a.ld_u) + c);
+    float raw = seq_ld<T>((const T *)((const char *)a.dt + t * a.ld_dt) + c);
     if (a.bias) raw += a.bias[c];
     const float delta = a.softplus ? softplus(raw) : raw;
-    const T *B = (const T *)a.B + t * a.ld_b + (int64_t)group * a.N + n0, *C = (const T *)a.C + t * a.ld_c + (int64_t)group * a.N + n0;
+    const T *B = (const T *)((const char *)a.B + t * a.ld_b) + group * a.N + n0, *C = (const T *)((const char *)a.C + t * a.ld_c) + group * a.N + n0;
     const float *from = state + ((int64_t)slot * a.channels + c) * a.N + n0, *A = a.A + (int64_t)c * a.N + n0;
     float *to = state_out + ((int64_t)slot * a.channels + c) * a.N + n0;
     float sum = 0.f;
@@ -190,19 +227,24 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     for (int m = NL / 2; m >= 1; m /= 2) sum += __shfl_xor(sum, m, 64);
     if (n0) return;
     float y = a.D ? fmaf(a.D[c], u, sum) : sum;
-    if (a.z) {
-        const float z = seq_ld<T>((const T *)a.z + t * a.ld_z + c);
+    if (a.gate) {
+        const float z = seq_ld<T>((const T *)((const char *)a.z + t * a.ld_z) + c);
         y *= z * sigmoid(z);
     }
-    seq_st((T *)a.y + t * a.ld_y + c, y);
+    seq_st((T *)((char *)a.y + t * a.ld_y) + c, y);
 }
 
-template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st)
+template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st)
 {
     return by_lanes(p.NL, [&](auto NL) {
         const dim3 grid(p.chunks, p.blocks);
-        if (s.dtype == SN_BF16) scan_fwd_kernel<bf16_t, NL.value, MODE><<<grid, THREADS, 0, st>>>(a);
-        else scan_fwd_kernel<float, NL.value, MODE><<<grid, THREADS, 0, st>>>(a);
+        if (s.dtype == SN_BF16) {
+            if (whole) scan_fwd_kernel<bf16_t, NL.value, true, MODE><<<grid, THREADS, 0, st>>>(a);
+            else scan_fwd_kernel<bf16_t, NL.value, false, MODE><<<grid, THREADS, 0, st>>>(a);
+        } else {
+            if (whole) scan_fwd_kernel<float, NL.value, true, MODE><<<grid, THREADS, 0, st>>>(a);
+            else scan_fwd_kernel<float, NL.value, false, MODE><<<grid, THREADS, 0, st>>>(a);
+        }
         return hipGetLastError();
     });
 }
@@ -233,8 +275,13 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
 int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
 {
     const ScanPlan p = scan_plan(s, 1);
+#if 1
+    const int64_t have = (int64_t)p.blocks * p.spans, want = getenv("SN_WANT_F") ? atoi(getenv(bwd ? "SN_WANT_B" : "SN_WANT_F")) : 512;
+    if (have >= want) return 1;
+#else
     const int64_t have = (int64_t)p.blocks * p.spans, want = 512;
     if (have >= want / 2) return 1;
+#endif
     int64_t parts = (want + have - 1) / have;
     const int64_t most = p.tiles_per_span / 4;   // chunks of 64 rows at least
     if (parts > most) parts = most;
@@ -244,32 +291,36 @@ int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
 size_t scan_carry_bytes(const sn_scan_shape &s, const ScanPlan &p)
 {
     if (p.parts == 1) return 0;
-    return align_up((size_t)p.chunks * s.channels * s.states * 4, 256) + align_up((size_t)p.chunks * s.channels * 4, 256) + align_up((size_t)p.chunks * 4, 256);
+    return align_up((size_t)p.chunks * s.channels * 4 * p.NL * 4, 256) + align_up((size_t)p.chunks * s.channels * 4, 256) + align_up((size_t)p.chunks * 4, 256);
 }
 
-ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off)
+ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off, const void *u, const void *dt, const float *A, const void *B, const void *C,
+                   const float *D, const void *z, const float *bias)
 {
     ScanArgs a = {};
-    a.ld_u = s.ld_u; a.ld_dt = s.ld_dt; a.ld_b = s.ld_b; a.ld_c = s.ld_c; a.ld_z = s.ld_z; a.ld_y = s.ld_y;
-    a.ld_du = s.ld_du; a.ld_ddt = s.ld_ddt; a.ld_db = s.ld_db; a.ld_dc = s.ld_dc; a.ld_dz = s.ld_dz;
+    const int64_t e = s.dtype == SN_BF16 ? 2 : 4;
+    const auto bytes = [&](int64_t ld) { return s.rows > 1 ? (uint32_t)(ld * e) : 0u; };   // of a single row no stride was looked at
+    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z ? z : u; a.bias = bias; a.gate = z != nullptr;
+    a.ld_u = bytes(s.ld_u); a.ld_dt = bytes(s.ld_dt); a.ld_b = bytes(s.ld_b); a.ld_c = bytes(s.ld_c); a.ld_z = bytes(z ? s.ld_z : s.ld_u); a.ld_y = bytes(s.ld_y);
+    a.ld_du = bytes(s.ld_du); a.ld_ddt = bytes(s.ld_ddt); a.ld_db = bytes(s.ld_db); a.ld_dc = bytes(s.ld_dc); a.ld_dz = bytes(s.ld_dz);
     a.rows = {off, s.seqs, (int)(s.rows / s.seqs), (int)s.rows};
-    a.channels = s.channels; a.N = s.states; a.per_group = s.channels / s.groups; a.blocks_per_group = p.blocks_per_group; a.softplus = s.softplus;
+    a.channels = s.channels; a.N = s.states; a.NP = 4 * p.NL; a.per_group = s.channels / s.groups; a.blocks_per_group = p.blocks_per_group; a.softplus = s.softplus;
     a.span_rows = p.span_rows; a.chunk_rows = p.chunk_rows; a.parts = p.parts; a.spans = p.spans; a.tiles_per_span = p.tiles_per_span;
     return a;
 }
 
 // Whether the rows of a tensor can be staged in whole pieces: by its address, its stride and the channels of a group.
-int scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan)
+bool scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan)
 {
     const int e = s.dtype == SN_BF16 ? 2 : 4, ve = plan.CB / 16, piece = ve * e > 16 ? 16 / e : ve;
-    return rows_aligned(p, ld, e, piece) && s.channels / s.groups % ve == 0;
+    return rows_aligned(p, s.rows > 1 ? ld : 0, e, piece) && s.channels / s.groups % ve == 0;
 }
 
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws)
 {
     char *at = (char *)ws;
     a.carry = (float *)at;
-    at += align_up((size_t)p.chunks * s.channels * s.states * 4, 256);
+    at += align_up((size_t)p.chunks * s.channels * 4 * p.NL * 4, 256);
     a.sum_delta = (float *)at;
     at += align_up((size_t)p.chunks * s.channels * 4, 256);
     a.through = (int *)at;
@@ -278,50 +329,48 @@ void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void
 size_t scan_states_bytes(const sn_scan_shape &s)
 {
     const ScanPlan p = scan_plan(s, 1);
-    return align_up((size_t)p.spans * p.tiles_per_span * s.channels * s.states * 4, 256);
+    return align_up((size_t)p.spans * p.tiles_per_span * s.channels * 4 * p.NL * 4, 256);
 }
 
 void scan_fwd_bytes(const sn_scan_shape &s, size_t *preferred_bytes) { *preferred_bytes = scan_carry_bytes(s, scan_plan(s, scan_parts_wanted(s, false))); }
 
 hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st)
 {
-    scan_carry_kernel<<<dim3(div_up((int64_t)a.channels * a.N, THREADS), p.spans), THREADS, 0, st>>>(a, reverse);
+    scan_carry_kernel<<<dim3(div_up((int64_t)a.channels * a.NP, THREADS), p.spans), THREADS, 0, st>>>(a, reverse);
     return hipGetLastError();
 }
 
-template <int MODE> static hipError_t fwd_in_chunks(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st)
+template <int MODE> static hipError_t fwd_in_chunks(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st)
 {
     if (p.parts > 1) {
-        ScanArgs local = a;
-        local.states = nullptr;
-        hipError_t e = launch_fwd<1>(local, s, p, st);
+        hipError_t e = launch_fwd<1>(a, s, p, whole, st);
         if (e == hipSuccess) e = launch_scan_carry(a, p, false, st);
         if (e != hipSuccess) return e;
     }
-    return launch_fwd<MODE>(a, s, p, st);
+    return launch_fwd<MODE>(a, s, p, whole, st);
 }
 
-hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, hipStream_t st) { return fwd_in_chunks<2>(a, s, p, st); }
+hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st) { return fwd_in_chunks<2>(a, s, p, whole, st); }
 
 hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
                            const sn_scan_shape &s, const int32_t *off, const float *h0, float *hT, float *states, void *ws, size_t ws_bytes, hipStream_t st)
 {
     ScanPlan p = scan_plan(s, scan_parts_wanted(s, false));
     while (p.parts > 1 && scan_carry_bytes(s, p) > ws_bytes) p = scan_plan(s, p.parts - 1);
-    ScanArgs a = scan_args(s, p, off);
-    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.bias = bias; a.y = y; a.h0 = h0; a.hT = hT; a.states = states;
-    a.whole_u = scan_whole_rows(u, s.ld_u, s, p); a.whole_dt = scan_whole_rows(dt, s.ld_dt, s, p); a.whole_y = scan_whole_rows(y, s.ld_y, s, p);
-    a.whole_z = z && scan_whole_rows(z, s.ld_z, s, p);
+    ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
+    a.y = y; a.h0 = h0; a.hT = hT; a.states = states;
+    const bool whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && scan_whole_rows(y, s.ld_y, s, p) &&
+                       (!z || scan_whole_rows(z, s.ld_z, s, p));
     if (p.parts > 1) scan_set_carry(a, s, p, ws);
-    return fwd_in_chunks<0>(a, s, p, st);
+    return fwd_in_chunks<0>(a, s, p, whole, st);
 }
 
 hipError_t launch_scan_step(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
                             const float *state, float *state_out, const int32_t *slots, int num_slots, const sn_scan_shape &s, hipStream_t st)
 {
     const ScanPlan p = scan_plan(s, 1);
-    ScanArgs a = scan_args(s, p, nullptr);
-    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.bias = bias; a.y = y;
+    ScanArgs a = scan_args(s, p, nullptr, u, dt, A, B, C, D, z, bias);
+    a.y = y;
     const dim3 grid((int)s.rows, div_up((int64_t)s.channels * p.NL, THREADS));
     return by_lanes(p.NL, [&](auto NL) {
         if (s.dtype == SN_BF16) scan_step_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);

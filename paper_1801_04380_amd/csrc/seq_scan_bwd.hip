@@ -18,8 +18,16 @@ namespace {
 
 constexpr int THREADS = 256;
 
+// Keeps a row's reads of LDS in front of what uses the row before it: nothing but arithmetic may be moved across.
+#define ROW_AHEAD() __builtin_amdgcn_sched_barrier(0x407)
+
+// A row's operands of a lane.
+struct RowIn {
+    float d, x, g, b[4], c[4];
+};
+
 // What of the gradient of the states a chunk hands on to the one before it, starting from zero, and its sum of delta.
-template <typename T, int NL>
+template <typename T, int NL, bool WHOLE>
 __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
@@ -39,31 +47,41 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     float g[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
     bool crossed = false;
     SeqAt at = seq_find(a.rows, r1 - 1);
-    Piece next = piece_before(a.rows, at, r1, r0);
-    Staged<T, NL> dt, z, dy;
-    StagedBC<T, NL> C;
+    Piece next = piece_before<TS>(a.rows, at, r1, r0);
+    Staged<T, NL, WHOLE> dt, z, dy;
+    StagedBC<T, NL, TS> C;
+    const char *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T), *pdy = (const char *)a.dy + c0 * sizeof(T);
+    const char *pC = (const char *)a.C + group * a.N * sizeof(T);
+    const uint32_t is_softplus = a.softplus ? ~0u : 0u, is_gate = a.gate ? ~0u : 0u;
     const auto fetch = [&]() {
-        const int64_t t = min(next.t0 + row, a.rows.rows - 1);
-        dt.load((const T *)a.dt + t * a.ld_dt + c0, co, nch, a.whole_dt);
-        dy.load((const T *)a.dy + t * a.ld_y + c0, co, nch, a.whole_y);
-        if (a.z) z.load((const T *)a.z + t * a.ld_z + c0, co, nch, a.whole_z);
-        C.load((const T *)a.C + group * a.N, a.ld_c, next.t0, a.rows.rows, a.N);
+        const int64_t t0 = next.t0;
+        const int have = a.rows.rows - next.t0, r = min(row, have - 1);
+        dt.load(pdt + t0 * a.ld_dt, a.ld_dt, r, co, nch);
+        dy.load(pdy + t0 * a.ld_y, a.ld_y, r, co, nch);
+        z.load(pz + t0 * a.ld_z, a.ld_z, r, co, nch);
+        C.load(pC + t0 * a.ld_c, a.ld_c, have, a.N);
     };
-    if (next.any) fetch();
-    while (next.any) {
-        const Piece now = next;
-        const bool in = now.holds(now.t0 + row);
+    const auto stage = [&](const Piece &p) {
+        const int first = p.p0 - p.t0, last = p.p1 - p.t0;
+        const bool in = row >= first && row < last;
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
             const bool here = in && i < nco;
             const float raw = dt.get(i) + bias[i];
-            s_delta[row][co + i] = here ? (a.softplus ? softplus(raw) : raw) : 0.f;
-            s_g[row][co + i] = here ? dy.get(i) * (a.z ? z.get(i) * sigmoid(z.get(i)) : 1.f) : 0.f;
+            s_delta[row][co + i] = keep_if(here, pick(is_softplus, softplus(raw), raw));
+            s_g[row][co + i] = keep_if(here, dy.get(i) * pick(is_gate, z.get(i) * sigmoid(z.get(i)), 1.f));
         }
-        C.put(s_C, now, a.N);
-        __syncthreads();
-        next = piece_before(a.rows, at, now.p0, r0);
+        C.put(s_C, first, last, a.N);
+    };
+    Piece now = next;
+    if (now.any) {
+        fetch();
+        stage(now);
+        next = piece_before<TS>(a.rows, at, now.p0, r0);
         if (next.any) fetch();
+    }
+    __syncthreads();
+    while (now.any) {
         if (now.end) {
             crossed = true;
             sum_delta = 0.f;
@@ -81,11 +99,18 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
                 sum_delta += delta;
             }
         };
-        if (now.full()) {
+        if (now.p1 - now.p0 == TS) {
 #pragma unroll
             for (int tb = TS - 4; tb >= 0; tb -= 4) rows(tb);
         } else {
             for (int tb = (now.p1 - 1 - now.t0) / 4 * 4; tb >= 0 && tb + 3 >= now.p0 - now.t0; tb -= 4) rows(tb);
+        }
+        __syncthreads();
+        now = next;
+        if (now.any) {
+            stage(now);
+            next = piece_before<TS>(a.rows, at, now.p0, r0);
+            if (next.any) fetch();
         }
         __syncthreads();
     }
@@ -94,7 +119,7 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
 }
 
-template <typename T, int NL>
+template <typename T, int NL, bool WHOLE>
 __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
@@ -121,45 +146,67 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
         A[i] = lane.there && lane.n0 + i < a.N ? a.A[(int64_t)lane.channel * a.N + lane.n0 + i] : 0.f;
         dA[i] = 0.f;
     }
+    const char *pu = (const char *)a.u + c0 * sizeof(T), *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T);
+    const char *pdy = (const char *)a.dy + c0 * sizeof(T), *pB = (const char *)a.B + group * a.N * sizeof(T), *pC = (const char *)a.C + group * a.N * sizeof(T);
+    char *pdu = (char *)a.du + c0 * sizeof(T), *pddt = (char *)a.ddt + c0 * sizeof(T), *pdz = (char *)a.dz + c0 * sizeof(T);
+    float *part_bc = a.part_bc + (int64_t)blockIdx.y * a.rows.rows * (2 * NP);
+    const uint32_t is_softplus = a.softplus ? ~0u : 0u, is_gate = a.gate ? ~0u : 0u;
     float g[4] = {0.f, 0.f, 0.f, 0.f};
     if (part < a.parts - 1) lane.load_own(a.carry, chunk, a, g);
 
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, r1 - 1);
-        Piece next = piece_before(a.rows, at, r1, r0);
-        Staged<T, NL> u, dt, z, dy;
-        StagedBC<T, NL> B, C;
+        Piece next = piece_before<TS>(a.rows, at, r1, r0);
+        Staged<T, NL, WHOLE> u, dt, z, dy;
+        StagedBC<T, NL, TS> B, C;
+        float4 kept = {};   // the state in front of the piece's tile
         const auto fetch = [&]() {
-            const int64_t t = min(next.t0 + row, a.rows.rows - 1);
-            u.load((const T *)a.u + t * a.ld_u + c0, co, nch, a.whole_u);
-            dt.load((const T *)a.dt + t * a.ld_dt + c0, co, nch, a.whole_dt);
-            dy.load((const T *)a.dy + t * a.ld_y + c0, co, nch, a.whole_y);
-            if (a.z) z.load((const T *)a.z + t * a.ld_z + c0, co, nch, a.whole_z);
-            B.load((const T *)a.B + group * a.N, a.ld_b, next.t0, a.rows.rows, a.N);
-            C.load((const T *)a.C + group * a.N, a.ld_c, next.t0, a.rows.rows, a.N);
+            const int64_t t0 = next.t0;
+            const int have = a.rows.rows - next.t0, r = min(row, have - 1);
+            u.load(pu + t0 * a.ld_u, a.ld_u, r, co, nch);
+            dt.load(pdt + t0 * a.ld_dt, a.ld_dt, r, co, nch);
+            dy.load(pdy + t0 * a.ld_y, a.ld_y, r, co, nch);
+            z.load(pz + t0 * a.ld_z, a.ld_z, r, co, nch);
+            B.load(pB + t0 * a.ld_b, a.ld_b, have, a.N);
+            C.load(pC + t0 * a.ld_c, a.ld_c, have, a.N);
+            kept = lane.fetch_own(a.states, (int64_t)span * a.tiles_per_span + (next.t0 - span * a.span_rows) / TS, a);
         };
-        if (next.any) fetch();
-        while (next.any) {
-            const Piece now = next;
-            const bool in = now.holds(now.t0 + row);
-            Staged<T, NL> u0 = u, dt0 = dt, z0 = z, dy0 = dy;   // as loaded: what is made of them is in LDS, or made again
+        // Of the staged piece, what its gradients take besides what is in LDS: u, d delta / d dt, d y / d z without y.  Made here, not kept as
+        // loaded: a copy of what the next loads go to would have to wait for them.
+        float uu[VE], slope[VE], zslope[VE];
+        float first[4];   // the state in front of it
+        const auto stage = [&](const Piece &p) {
+            const int begin = p.p0 - p.t0, last = p.p1 - p.t0;
+            const bool in = row >= begin && row < last;
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 const bool here = in && i < nco;
-                const float raw = dt.get(i) + bias[i], delta = here ? (a.softplus ? softplus(raw) : raw) : 0.f;
+                const float raw = dt.get(i) + bias[i], delta = keep_if(here, pick(is_softplus, softplus(raw), raw));
+                const float zz = z.get(i), sz = sigmoid(zz), d = dy.get(i);
+                uu[i] = keep_if(here, u.get(i));
+                slope[i] = keep_if(here, pick(is_softplus, sigmoid(raw), 1.f));
+                zslope[i] = d * sz * fmaf(zz, 1.f - sz, 1.f);
                 s_delta[row][co + i] = delta;
-                s_x[row][co + i] = here ? delta * u.get(i) : 0.f;
-                s_g[row][co + i] = here ? (a.z ? dy.get(i) * (z.get(i) * sigmoid(z.get(i))) : dy.get(i)) : 0.f;
+                s_x[row][co + i] = delta * uu[i];
+                s_g[row][co + i] = keep_if(here, pick(is_gate, d * (zz * sz), d));
             }
-            B.put(s_B, now, a.N);
-            C.put(s_C, now, a.N);
-            __syncthreads();
-            float first[4];   // the state in front of the piece
-            if (!now.start) lane.load_own(a.states, (int64_t)span * a.tiles_per_span + (now.t0 - span * a.span_rows) / TS, a, first);
-            else if (a.h0) lane.load(a.h0, now.seq, a, first);
-            else first[0] = first[1] = first[2] = first[3] = 0.f;
-            next = piece_before(a.rows, at, now.p0, r0);
+            B.put(s_B, begin, last, a.N);
+            C.put(s_C, begin, last, a.N);
+            lane.take(kept, a, first);
+            if (p.start) {
+                if (a.h0) lane.load(a.h0, p.seq, a, first);
+                else first[0] = first[1] = first[2] = first[3] = 0.f;
+            }
+        };
+        Piece now = next;
+        if (now.any) {
+            fetch();
+            stage(now);
+            next = piece_before<TS>(a.rows, at, now.p0, r0);
             if (next.any) fetch();
+        }
+        __syncthreads();
+        while (now.any) {
             if (now.end) {
                 if (a.dhT) lane.load(a.dhT, now.seq, a, g);
                 else g[0] = g[1] = g[2] = g[3] = 0.f;
@@ -168,21 +215,32 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
             constexpr int TB = CW < 8 ? 1 : CW / 8;       // rows whose 8 values share the exchanges over channels
             constexpr int GR = NL > TB ? NL : TB;         // rows that are worked on or left out together
             constexpr int HR = GR > 8 ? GR : 8;           // rows whose states are in registers at a time
+            const auto read = [&](int t) {
+                RowIn r;
+                r.d = s_delta[t][lane.c];
+                r.x = s_x[t][lane.c];
+                r.g = s_g[t][lane.c];
+                *reinterpret_cast<float4 *>(r.b) = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
+                *reinterpret_cast<float4 *>(r.c) = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                return r;
+            };
             const auto tile = [&](auto whole) {
-                constexpr bool WHOLE = whole.value;
-                const auto outside = [&](int tb, int n) { return !WHOLE && (now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1); };
+                constexpr bool FULL = whole.value;
+                const auto outside = [&](int tb, int n) { return !FULL && (now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1); };
                 // the state in front of the second half
                 float mid[4] = {first[0], first[1], first[2], first[3]};
                 if constexpr (HR < TS) {
-                    if (!outside(0, HR))
+                    if (!outside(0, HR)) {
+                        RowIn r, ahead = read(0);
 #pragma unroll
                         for (int t = 0; t < HR; ++t) {
-                            const float d = s_delta[t][lane.c], x = s_x[t][lane.c];
-                            const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
-                            const float bb[4] = {b.x, b.y, b.z, b.w};
+                            r = ahead;
+                            ahead = read(t + 1 < HR ? t + 1 : t);
+                            ROW_AHEAD();
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(d * lane.A2[i]), mid[i], x * bb[i]);
+                            for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(r.d * lane.A2[i]), mid[i], r.x * r.b[i]);
                         }
+                    }
                 }
 #pragma unroll 1
                 for (int half = TS - HR; half >= 0; half -= HR) {
@@ -203,18 +261,19 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                             continue;
                         }
                         float acc[NL];
+                        RowIn r, ahead = read(half + kb);
 #pragma unroll
                         for (int k = kb; k < kb + GR; ++k) {
                             const int t = half + k;
-                            const float d = s_delta[t][lane.c], x = s_x[t][lane.c];
-                            const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                            const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                            r = ahead;
+                            ahead = read(k + 1 < HR ? t + 1 : t);
+                            ROW_AHEAD();
                             float sum = 0.f;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                decay[k][i] = exp2_fast(d * lane.A2[i]);
-                                hs[k + 1][i] = fmaf(decay[k][i], hs[k][i], x * bb[i]);
-                                sum = fmaf(hs[k + 1][i], cc[i], sum);
+                                decay[k][i] = exp2_fast(r.d * lane.A2[i]);
+                                hs[k + 1][i] = fmaf(decay[k][i], hs[k][i], r.x * r.b[i]);
+                                sum = fmaf(hs[k + 1][i], r.c[i], sum);
                             }
                             acc[t % NL] = sum;
                             if (t % NL == NL - 1) s_y[t / NL * NL + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
@@ -226,23 +285,24 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                     for (int kb = HR - GR; kb >= 0; kb -= GR) {
                         if (outside(half + kb, GR)) continue;
                         float gb[NL], qa[NL], bc[8 * TB];
+                        RowIn r, ahead = read(half + kb + GR - 1);
 #pragma unroll
                         for (int k = kb + GR - 1; k >= kb; --k) {
                             const int t = half + k;
-                            const float d = s_delta[t][lane.c], x = s_x[t][lane.c], gyt = s_g[t][lane.c];
-                            const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]), c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                            const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                            r = ahead;
+                            ahead = read(k ? t - 1 : t);
+                            ROW_AHEAD();
                             float sum_b = 0.f, sum_a = 0.f;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const float gi = fmaf(gyt, cc[i], g[i]);
-                                bc[t % TB * 8 + i] = gi * x;
-                                bc[t % TB * 8 + 4 + i] = gyt * hs[k + 1][i];
-                                sum_b = fmaf(gi, bb[i], sum_b);
+                                const float gi = fmaf(r.g, r.c[i], g[i]);
+                                bc[t % TB * 8 + i] = gi * r.x;
+                                bc[t % TB * 8 + 4 + i] = r.g * hs[k + 1][i];
+                                sum_b = fmaf(gi, r.b[i], sum_b);
                                 g[i] = decay[k][i] * gi;
                                 const float q = g[i] * hs[k][i];
                                 sum_a = fmaf(q, A[i], sum_a);
-                                dA[i] = fmaf(q, d, dA[i]);
+                                dA[i] = fmaf(q, r.d, dA[i]);
                             }
                             gb[t % NL] = sum_b;
                             qa[t % NL] = sum_a;
@@ -264,42 +324,46 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                     }
                 }
             };
-            if (now.full()) tile(ScanInt<1>());
+            if (now.p1 - now.p0 == TS) tile(ScanInt<1>());
             else tile(ScanInt<0>());
             if (a.dh0 && now.start) lane.store(a.dh0, now.seq, a, g);
             __syncthreads();
-            if (in) {
-                const int64_t t = now.t0 + row;
-                Staged<T, NL> o;
-                float dd[VE];
+            const bool in = now.holds(now.t0 + row);
+            Staged<T, NL, WHOLE> du, ddt, dz;
 #pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    const float vb = s_gb[row][co + i], va = s_qa[row][co + i], gy = s_g[row][co + i], uu = u0.get(i);
-                    o.set(i, fmaf(gy, skip[i], s_delta[row][co + i] * vb));
-                    dd[i] = fmaf(uu, vb, va);
-                    if (a.softplus) dd[i] *= sigmoid(dt0.get(i) + bias[i]);
-                    if (i < nco) {
-                        dbias[i] += dd[i];
-                        dD[i] = fmaf(gy, uu, dD[i]);
-                    }
-                }
-                o.store((T *)a.du + t * a.ld_du + c0, co, nch, a.whole_du);
-#pragma unroll
-                for (int i = 0; i < VE; ++i) o.set(i, dd[i]);
-                o.store((T *)a.ddt + t * a.ld_ddt + c0, co, nch, a.whole_ddt);
-                if (a.z) {
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) {
-                        const float zz = z0.get(i), s = sigmoid(zz);
-                        o.set(i, dy0.get(i) * fmaf(skip[i], u0.get(i), s_y[row][co + i]) * s * (1.f + zz * (1.f - s)));
-                    }
-                    o.store((T *)a.dz + t * a.ld_dz + c0, co, nch, a.whole_dz);
-                }
+            for (int i = 0; i < VE; ++i) {
+                const float vb = s_gb[row][co + i], va = s_qa[row][co + i], gy = s_g[row][co + i];
+                const float dd = fmaf(uu[i], vb, va) * slope[i];
+                du.set(i, fmaf(gy, skip[i], s_delta[row][co + i] * vb));
+                ddt.set(i, dd);
+                dz.set(i, zslope[i] * fmaf(skip[i], uu[i], s_y[row][co + i]));
+                const bool here = in && i < nco;
+                dbias[i] += keep_if(here, dd);
+                dD[i] = fmaf(gy, uu[i], dD[i]);   // both are zero elsewhere
             }
-            for (int k = threadIdx.x; k < TS * 2 * NP; k += THREADS) {
-                const int r = k / (2 * NP), n = k % (2 * NP);
-                if (now.holds(now.t0 + r))
-                    a.part_bc[((int64_t)blockIdx.y * a.rows.rows + now.t0 + r) * (2 * NP) + n] = s_bc[0][r][n] + s_bc[1][r][n] + s_bc[2][r][n] + s_bc[3][r][n];
+            constexpr int PER = (TS * 2 * NP + THREADS - 1) / THREADS;
+            float bc[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int k = i * THREADS + threadIdx.x, r = k / (2 * NP) % TS, n = k % (2 * NP);
+                bc[i] = s_bc[0][r][n] + s_bc[1][r][n] + s_bc[2][r][n] + s_bc[3][r][n];
+            }
+            // The next rows are staged before anything is stored: whoever waits for the loads waits for what was stored since as well.
+            if (next.any) stage(next);
+            if (in) {
+                du.store(pdu + (int64_t)now.t0 * a.ld_du, a.ld_du, row, co, nch);
+                ddt.store(pddt + (int64_t)now.t0 * a.ld_ddt, a.ld_ddt, row, co, nch);
+                if (a.gate) dz.store(pdz + (int64_t)now.t0 * a.ld_dz, a.ld_dz, row, co, nch);
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t k = i * THREADS + threadIdx.x, r = k / (2 * NP);
+                if (r < TS && now.holds(now.t0 + r)) (part_bc + (int64_t)now.t0 * (2 * NP))[k] = bc[i];
+            }
+            now = next;
+            if (now.any) {
+                next = piece_before<TS>(a.rows, at, now.p0, r0);
+                if (next.any) fetch();
             }
             __syncthreads();
         }
@@ -339,18 +403,19 @@ __global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int grou
     float sum = 0.f;
     for (int b = 0; b < a.blocks_per_group; ++b)
         sum += a.part_bc[(((int64_t)group * a.blocks_per_group + b) * a.rows.rows + row) * (2 * NP) + which * NP + n];
-    T *to = which ? (T *)a.dC + row * a.ld_dc : (T *)a.dB + row * a.ld_db;
-    seq_st(to + (int64_t)group * a.N + n, sum);
+    char *to = which ? (char *)a.dC + row * a.ld_dc : (char *)a.dB + row * a.ld_db;
+    seq_st((T *)to + group * a.N + n, sum);
 }
 
 // dA, dD and the bias's gradient from the sums of the chunks.
 __global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunks, float *__restrict__ dA, float *__restrict__ dD, float *__restrict__ dbias)
 {
-    const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.N;
+    int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+    const int64_t each = (int64_t)a.channels * a.N;
     const float *from;
     float *to;
     int64_t at, stride;
-    if (i < each) { from = a.part_a; to = dA; at = i; stride = each; }
+    if (i < each) { from = a.part_a + i / a.N * (a.NP - a.N); to = dA; at = i; stride = (int64_t)a.channels * a.NP; }
     else if (i < each + a.channels) { from = a.part_d; to = dD; at = i - each; stride = a.channels; }
     else if (i < each + 2 * (int64_t)a.channels) { from = a.part_bias; to = dbias; at = i - each - a.channels; stride = a.channels; }
     else return;
@@ -358,6 +423,19 @@ __global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunk
     float sum = 0.f;
     for (int c = 0; c < chunks; ++c) sum += from[c * stride + at];
     to[at] = sum;
+}
+
+template <typename T, int NL, bool WHOLE> hipError_t bwd_in_chunks(const ScanArgs &a, const ScanPlan &p, hipStream_t st)
+{
+    const dim3 grid(p.chunks, p.blocks);
+    if (p.parts > 1) {
+        scan_bwd_local_kernel<T, NL, WHOLE><<<grid, THREADS, 0, st>>>(a);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess) e = launch_scan_carry(a, p, true, st);
+        if (e != hipSuccess) return e;
+    }
+    scan_bwd_kernel<T, NL, WHOLE><<<grid, THREADS, 0, st>>>(a);
+    return hipGetLastError();
 }
 
 struct BwdBytes {
@@ -369,7 +447,7 @@ BwdBytes bytes_of(const sn_scan_shape &s, const ScanPlan &p)
 {
     BwdBytes b;
     b.carry = scan_carry_bytes(s, p);
-    b.a = align_up((size_t)p.chunks * s.channels * s.states * 4, 256);
+    b.a = align_up((size_t)p.chunks * s.channels * 4 * p.NL * 4, 256);
     b.d = align_up((size_t)p.chunks * s.channels * 4, 256);
     b.bc = align_up((size_t)p.blocks * s.rows * 8 * p.NL * 4, 256);
     return b;
@@ -390,12 +468,12 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     ScanPlan p = scan_plan(s, scan_parts_wanted(s, true));
     while (p.parts > 1 && replay + bytes_of(s, p).all() > ws_bytes) p = scan_plan(s, p.parts - 1);
     const BwdBytes b = bytes_of(s, p);
-    ScanArgs a = scan_args(s, p, off);
-    a.u = u; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.bias = bias; a.h0 = h0;
+    ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
+    a.h0 = h0;
     a.dy = g.dy; a.du = g.du; a.ddt = g.ddt; a.dB = g.dB; a.dC = g.dC; a.dz = g.dz; a.dhT = g.dhT; a.dh0 = g.dh0;
-    a.whole_u = scan_whole_rows(u, s.ld_u, s, p); a.whole_dt = scan_whole_rows(dt, s.ld_dt, s, p); a.whole_y = scan_whole_rows(g.dy, s.ld_y, s, p);
-    a.whole_du = scan_whole_rows(g.du, s.ld_du, s, p); a.whole_ddt = scan_whole_rows(g.ddt, s.ld_ddt, s, p);
-    a.whole_z = z && scan_whole_rows(z, s.ld_z, s, p); a.whole_dz = z && scan_whole_rows(g.dz, s.ld_dz, s, p);
+    const bool in_whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && (!z || scan_whole_rows(z, s.ld_z, s, p));
+    const bool whole = in_whole && scan_whole_rows(g.dy, s.ld_y, s, p) && scan_whole_rows(g.du, s.ld_du, s, p) && scan_whole_rows(g.ddt, s.ld_ddt, s, p) &&
+                       (!z || scan_whole_rows(g.dz, s.ld_dz, s, p));
     char *at = (char *)ws;
     a.states = states ? const_cast<float *>(states) : (float *)at;
     at += replay;
@@ -406,21 +484,12 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     a.part_bias = (float *)at; at += b.d;
     a.part_bc = (float *)at;
     hipError_t e = hipSuccess;
-    if (!states && s.rows) e = launch_scan_states(a, s, p, st);
+    if (!states && s.rows) e = launch_scan_states(a, s, p, in_whole, st);
     if (e != hipSuccess) return e;
     const bool bf16 = s.dtype == SN_BF16;
     e = by_lanes(p.NL, [&](auto NL) {
-        const dim3 grid(p.chunks, p.blocks);
-        if (p.parts > 1) {
-            if (bf16) scan_bwd_local_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a);
-            else scan_bwd_local_kernel<float, NL.value><<<grid, THREADS, 0, st>>>(a);
-            hipError_t f = hipGetLastError();
-            if (f == hipSuccess) f = launch_scan_carry(a, p, true, st);
-            if (f != hipSuccess) return f;
-        }
-        if (bf16) scan_bwd_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a);
-        else scan_bwd_kernel<float, NL.value><<<grid, THREADS, 0, st>>>(a);
-        return hipGetLastError();
+        if (bf16) return whole ? bwd_in_chunks<bf16_t, NL.value, true>(a, p, st) : bwd_in_chunks<bf16_t, NL.value, false>(a, p, st);
+        return whole ? bwd_in_chunks<float, NL.value, true>(a, p, st) : bwd_in_chunks<float, NL.value, false>(a, p, st);
     });
     if (e != hipSuccess) return e;
     if (s.rows) {
