@@ -90,13 +90,14 @@ __device__ inline float exp_fast(float x) { return exp2_fast(x * 1.4426950408889
 __device__ inline float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ inline float sigmoid(float x) { return rcp_fast(1.f + exp_fast(-x)); }
 
-// log(1 + e^x).  log(u) for u = 1 + e^x as rounded, times e^x / (u - 1), which takes the rounding of u out again to first order (u - 1 is
-// exact); from 20 on log(1 + e^-x) is below half a step of x.
+// log(1 + e^x).  With u = 1 + e^x as rounded, log(1 + e^x) = log(u) + (e^x - (u - 1)) / u to first order in what the rounding lost, and u - 1 is
+// exact.  Below u = 4 the division is left out (what was lost is half a step of u at most, 2^-23: the result is off by less than 2^-23 * 3/4 of
+// log(4), and by nothing to speak of near u = 1, where it counts); from there on the whole correction, below 2^-24 of a result above log(4).  From 20
+// on log(1 + e^-x) is below half a step of x.
 __device__ inline float softplus(float x)
 {
-    const float e = exp_fast(x), u = 1.f + e, d = u - 1.f;
-    const float l = __builtin_amdgcn_logf(u) * 0.69314718055994530942f;
-    const float r = d == 0.f ? e : l * (e * rcp_fast(d));
+    const float e = exp_fast(x), u = 1.f + e;
+    const float r = __builtin_amdgcn_logf(u) * 0.69314718055994530942f + (u < 4.f ? e - (u - 1.f) : 0.f);
     return x > 20.f ? x : r;
 }
 

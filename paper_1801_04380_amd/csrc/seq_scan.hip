@@ -8,7 +8,6 @@
 // final state from a zero one and its sum of delta (the product of its decays is exp(A * sum)), scan_carry_kernel joins them, and the
 // second pass starts each chunk from its state.
 #include "seq_scan.h"
-#include <cstdlib>
 
 namespace sn {
 namespace {
@@ -108,33 +107,40 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
                 keep(0);
             }
 
-            const auto rows = [&](int tb) {   // NL rows, and the sums of their outputs
+            // GR rows at a time, those of them that are not the piece's doing nothing; a row's operands are read while the one before it is worked on
+            constexpr int GR = NL > 4 ? NL : 4;
+            struct RowIn {
+                float d, x, b[4], c[4];
+            };
+            const auto read = [&](int t) {
+                RowIn r;
+                r.d = s_delta[t][lane.c];
+                r.x = s_x[t][lane.c];
+                *reinterpret_cast<float4 *>(r.b) = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
+                if (OUT) *reinterpret_cast<float4 *>(r.c) = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                return r;
+            };
+            const int tb0 = (now.p0 - now.t0) / GR * GR;
+            RowIn r, ahead = read(tb0);
+#pragma unroll 1
+            for (int tb = tb0; tb < now.p1 - now.t0; tb += GR) {
                 if (!LOCAL && a.states && tb && tb % TS == 0 && now.t0 + tb > now.p0) keep(tb);
                 float acc[NL];
 #pragma unroll
-                for (int k = 0; k < NL; ++k) {
-                    const int t = tb + k;
-                    const float delta = s_delta[t][lane.c], x = s_x[t][lane.c];
-                    const float4 b = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
-                    float4 c = {};
-                    if (OUT) c = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                    const float bb[4] = {b.x, b.y, b.z, b.w}, cc[4] = {c.x, c.y, c.z, c.w};
+                for (int k = 0; k < GR; ++k) {
+                    r = ahead;
+                    ahead = read(k + 1 < GR ? tb + k + 1 : min(tb + GR, ROWS - 1));
+                    __builtin_amdgcn_sched_barrier(0x407);   // the reads stay in front: nothing but arithmetic may be moved across
                     float sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        h[i] = fmaf(exp2_fast(delta * lane.A2[i]), h[i], x * bb[i]);
-                        sum = fmaf(h[i], cc[i], sum);
+                        h[i] = fmaf(exp2_fast(r.d * lane.A2[i]), h[i], r.x * r.b[i]);
+                        if (OUT) sum = fmaf(h[i], r.c[i], sum);
                     }
-                    acc[k] = sum;
-                    if (LOCAL) sum_delta += delta;
+                    acc[k % NL] = sum;
+                    if (LOCAL) sum_delta += r.d;
+                    if (OUT && k % NL == NL - 1) s_y[tb + k / NL * NL + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
                 }
-                if (OUT) s_y[tb + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
-            };
-            if (now.p1 - now.p0 == ROWS) {
-#pragma unroll
-                for (int tb = 0; tb < ROWS; tb += NL) rows(tb);
-            } else {
-                for (int tb = (now.p0 - now.t0) / NL * NL; tb < now.p1 - now.t0; tb += NL) rows(tb);
             }
             if (OUT && a.hT && now.end) lane.store(a.hT, now.seq, a, h);
             __syncthreads();
@@ -275,13 +281,8 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
 int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
 {
     const ScanPlan p = scan_plan(s, 1);
-#if 1
-    const int64_t have = (int64_t)p.blocks * p.spans, want = getenv("SN_WANT_F") ? atoi(getenv(bwd ? "SN_WANT_B" : "SN_WANT_F")) : 512;
+    const int64_t have = (int64_t)p.blocks * p.spans, want = bwd ? 512 : 1024;
     if (have >= want) return 1;
-#else
-    const int64_t have = (int64_t)p.blocks * p.spans, want = 512;
-    if (have >= want / 2) return 1;
-#endif
     int64_t parts = (want + have - 1) / have;
     const int64_t most = p.tiles_per_span / 4;   // chunks of 64 rows at least
     if (parts > most) parts = most;

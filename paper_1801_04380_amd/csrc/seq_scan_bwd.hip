@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
     constexpr int CB = G::CB, NP = G::NP, VE = G::VE, CW = G::CW;
-    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_g[TS][CB], s_y[TS][CB], s_gb[TS][CB], s_qa[TS][CB];
+    __shared__ float s_delta[TS][CB], s_x[TS][CB], s_g[TS][CB], s_y[TS][CB], s_qa[TS][CB], s_dD[TS][CB], s_dbias[TS][CB], s_bias[CB], s_skip[CB];
     __shared__ alignas(16) float s_B[TS * NP], s_C[TS * NP];
     __shared__ float s_bc[4][TS][2 * NP];
 
@@ -134,18 +134,17 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
     const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
     const ScanLane<NL> lane(a, c0, nch);
     const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = scan_lane() % NL, wave = threadIdx.x / 64;
-    float bias[VE], skip[VE], dD[VE], dbias[VE], A[4], dA[4];
+    float dA[4];   // of what a thread stages, bias, D and their gradients' sums are in LDS: registers decide how many waves a SIMD has
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
-        bias[i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
-        skip[i] = a.D && i < nco ? a.D[c0 + co + i] : 0.f;
-        dD[i] = dbias[i] = 0.f;
+        s_dD[row][co + i] = s_dbias[row][co + i] = 0.f;
+        if (row) continue;
+        s_bias[co + i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
+        s_skip[co + i] = a.D && i < nco ? a.D[c0 + co + i] : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        A[i] = lane.there && lane.n0 + i < a.N ? a.A[(int64_t)lane.channel * a.N + lane.n0 + i] : 0.f;
-        dA[i] = 0.f;
-    }
+    for (int i = 0; i < 4; ++i) dA[i] = 0.f;
+    __syncthreads();
     const char *pu = (const char *)a.u + c0 * sizeof(T), *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T);
     const char *pdy = (const char *)a.dy + c0 * sizeof(T), *pB = (const char *)a.B + group * a.N * sizeof(T), *pC = (const char *)a.C + group * a.N * sizeof(T);
     char *pdu = (char *)a.du + c0 * sizeof(T), *pddt = (char *)a.ddt + c0 * sizeof(T), *pdz = (char *)a.dz + c0 * sizeof(T);
@@ -181,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 const bool here = in && i < nco;
-                const float raw = dt.get(i) + bias[i], delta = keep_if(here, pick(is_softplus, softplus(raw), raw));
+                const float raw = dt.get(i) + s_bias[co + i], delta = keep_if(here, pick(is_softplus, softplus(raw), raw));
                 const float zz = z.get(i), sz = sigmoid(zz), d = dy.get(i);
                 uu[i] = keep_if(here, u.get(i));
                 slope[i] = keep_if(here, pick(is_softplus, sigmoid(raw), 1.f));
@@ -224,22 +223,19 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                 *reinterpret_cast<float4 *>(r.c) = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
                 return r;
             };
-            const auto tile = [&](auto whole) {
-                constexpr bool FULL = whole.value;
-                const auto outside = [&](int tb, int n) { return !FULL && (now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1); };
+            const auto outside = [&](int tb, int n) { return now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1; };
+            {
                 // the state in front of the second half
                 float mid[4] = {first[0], first[1], first[2], first[3]};
-                if constexpr (HR < TS) {
-                    if (!outside(0, HR)) {
-                        RowIn r, ahead = read(0);
+                if (HR < TS && !outside(0, HR)) {
+                    RowIn r, ahead = read(0);
 #pragma unroll
-                        for (int t = 0; t < HR; ++t) {
-                            r = ahead;
-                            ahead = read(t + 1 < HR ? t + 1 : t);
-                            ROW_AHEAD();
+                    for (int t = 0; t < HR; ++t) {
+                        r = ahead;
+                        ahead = read(t + 1 < HR ? t + 1 : t);
+                        ROW_AHEAD();
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(r.d * lane.A2[i]), mid[i], r.x * r.b[i]);
-                        }
+                        for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(r.d * lane.A2[i]), mid[i], r.x * r.b[i]);
                     }
                 }
 #pragma unroll 1
@@ -301,13 +297,13 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                                 sum_b = fmaf(gi, r.b[i], sum_b);
                                 g[i] = decay[k][i] * gi;
                                 const float q = g[i] * hs[k][i];
-                                sum_a = fmaf(q, A[i], sum_a);
+                                sum_a = fmaf(q, lane.A2[i], sum_a);
                                 dA[i] = fmaf(q, r.d, dA[i]);
                             }
                             gb[t % NL] = sum_b;
                             qa[t % NL] = sum_a;
                             if (t % NL == 0) {   // rows t .. t + NL - 1 are done
-                                s_gb[t + nl][lane.c] = scatter_sum<NL / 2, 1>(gb);
+                                s_x[t + nl][lane.c] = scatter_sum<NL / 2, 1>(gb);   // over what the rows were staged with
                                 s_qa[t + nl][lane.c] = scatter_sum<NL / 2, 1>(qa);
                             }
                             if (t % TB == 0) {
@@ -323,23 +319,21 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                         }
                     }
                 }
-            };
-            if (now.p1 - now.p0 == TS) tile(ScanInt<1>());
-            else tile(ScanInt<0>());
+            }
             if (a.dh0 && now.start) lane.store(a.dh0, now.seq, a, g);
             __syncthreads();
             const bool in = now.holds(now.t0 + row);
             Staged<T, NL, WHOLE> du, ddt, dz;
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                const float vb = s_gb[row][co + i], va = s_qa[row][co + i], gy = s_g[row][co + i];
+                const float vb = s_x[row][co + i], va = s_qa[row][co + i] * 0.69314718055994530942f /* A is A2 * ln 2 */, gy = s_g[row][co + i];
                 const float dd = fmaf(uu[i], vb, va) * slope[i];
-                du.set(i, fmaf(gy, skip[i], s_delta[row][co + i] * vb));
+                du.set(i, fmaf(gy, s_skip[co + i], s_delta[row][co + i] * vb));
                 ddt.set(i, dd);
-                dz.set(i, zslope[i] * fmaf(skip[i], uu[i], s_y[row][co + i]));
+                dz.set(i, zslope[i] * fmaf(s_skip[co + i], uu[i], s_y[row][co + i]));
                 const bool here = in && i < nco;
-                dbias[i] += keep_if(here, dd);
-                dD[i] = fmaf(gy, uu[i], dD[i]);   // both are zero elsewhere
+                s_dbias[row][co + i] += keep_if(here, dd);
+                s_dD[row][co + i] = fmaf(gy, uu[i], s_dD[row][co + i]);   // both are zero elsewhere
             }
             constexpr int PER = (TS * 2 * NP + THREADS - 1) / THREADS;
             float bc[PER];
@@ -370,17 +364,13 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
     }
     lane.store_own(a.part_a, chunk, a, dA);
     // dD and the bias's gradient: over the 16 threads that stage a channel
-    for (int what = 0; what < 2; ++what) {
-        __syncthreads();
+    __syncthreads();
+    for (int k = threadIdx.x; k < 2 * CB; k += THREADS) {
+        const int c = k % CB;
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < VE; ++i) s_x[row][co + i] = what ? dbias[i] : dD[i];
-        __syncthreads();
-        for (int c = threadIdx.x; c < nch; c += THREADS) {
-            float sum = 0.f;
-#pragma unroll
-            for (int r = 0; r < TS; ++r) sum += s_x[r][c];
-            (what ? a.part_bias : a.part_d)[(int64_t)chunk * a.channels + c0 + c] = sum;
-        }
+        for (int r = 0; r < TS; ++r) sum += k < CB ? s_dD[r][c] : s_dbias[r][c];
+        if (c < nch) (k < CB ? a.part_d : a.part_bias)[(int64_t)chunk * a.channels + c0 + c] = sum;
     }
     if (a.dh0 && chunk == 0 && (a.rows.off || a.rows.rows == 0))
         for (int s = 0; s < a.rows.seqs; ++s) {   // through empty sequences
