@@ -8,7 +8,7 @@ import ctypes
 import torch
 
 from . import _lib
-from .api import SN_BF16, SN_F32, _check, _dtype_code, _stream
+from .api import SN_BF16, _check, _dtype_code
 
 __all__ = [
     "sn_causal_conv1d_fwd", "sn_causal_conv1d_scratch_bytes", "sn_causal_conv1d_bwd", "sn_causal_conv1d_step",
@@ -70,67 +70,79 @@ def _fn(name):
 
 
 def _call(name, *args):
-    _check(name, _fn(name)(*args))
+    status = (_fns.get(name) or _fn(name))(*args)
+    if status:
+        _check(name, status)
 
 
-def _here(t, what):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+# The checks are the larger part of what a small call costs the host: one look at each attribute, messages only when something is wrong.
+def _device(t, what):
+    """-> the current device, on which t has to live."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError("%s: expected a tensor on the current device" % what)
+    return t.get_device()
 
 
-def _rows(t, rows, width, dtype, what):
-    """-> (pointer, row stride) of a (rows, width) token tensor."""
-    _here(t, what)
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.dtype != dtype:
-        raise ValueError("%s: expected a (%d, %d) tensor of %s, got %s of %s" % (what, rows, width, dtype, tuple(t.shape), t.dtype))
-    if width > 1 and t.stride(1) != 1:
+def _stream_of(device):
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _refuse(t, shape, dtype, what, device, how):
+    if not t.is_cuda or t.get_device() != device:
+        raise ValueError("%s: expected a tensor on the current device" % what)
+    raise ValueError("%s: expected a %s %s tensor of %s, got %s of %s" % (what, how, tuple(shape), dtype, tuple(t.shape), t.dtype))
+
+
+def _rows(t, shape, dtype, what, device):
+    """-> (pointer, row stride) of a token tensor of that shape."""
+    if t.get_device() != device or t.shape != shape or t.dtype is not dtype:
+        _refuse(t, shape, dtype, what, device, "two-dimensional")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
         raise ValueError("%s: the channels of a row have to be contiguous" % what)
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), ld
 
 
-def _dense(t, shape, dtype, what):
+def _dense(t, shape, dtype, what, device):
     """-> pointer of a contiguous tensor of that shape, None for None."""
     if t is None:
         return None
-    _here(t, what)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError("%s: expected a contiguous %s tensor of %s, got %s of %s" % (what, tuple(shape), dtype, tuple(t.shape), t.dtype))
+    if t.get_device() != device or t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        _refuse(t, shape, dtype, what, device, "contiguous")
     return t.data_ptr()
 
 
-def _bytes(t, what):
+def _bytes(t, what, device):
     if t is None:
         return None, 0
-    _here(t, what)
-    if not t.is_contiguous():
-        raise ValueError("%s: expected a contiguous tensor" % what)
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse(t, t.shape, t.dtype, what, device, "contiguous")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _offsets(offsets, seqs):
-    return _dense(offsets, (seqs + 1,), torch.int32, "offsets")
-
-
-def _slots(slots, rows):
-    return _dense(slots, (rows,), torch.int32, "slots")
+_f32, _int32 = torch.float32, torch.int32
 
 
 # ---- short causal convolution ----
 def _conv1d_shape(x, w, y, what, seqs, silu, dx=None):
-    rows, channels = x.shape
+    device, t = _device(x, "x"), x.dtype
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x has to be (rows, channels), w (channels, width)")
+    shape = x.shape
+    rows, channels = shape
     width = w.shape[1]
-    xp, ldx = _rows(x, rows, channels, x.dtype, "x")
-    yp, ldy = _rows(y, rows, channels, x.dtype, what)
-    dxp, lddx = _rows(dx, rows, channels, x.dtype, "dx") if dx is not None else (None, 0)
-    wp = _dense(w, (channels, width), x.dtype, "w")
-    return xp, wp, yp, dxp, Conv1dShape(rows, seqs, channels, width, int(bool(silu)), _dtype_code(x), ldx, ldy, lddx)
+    xp, ldx = _rows(x, shape, t, "x", device)
+    yp, ldy = _rows(y, shape, t, what, device)
+    dxp, lddx = _rows(dx, shape, t, "dx", device) if dx is not None else (None, 0)
+    wp = _dense(w, (channels, width), t, "w", device)
+    return device, xp, wp, yp, dxp, Conv1dShape(rows, seqs, channels, width, 1 if silu else 0, _dtype_code(x), ldx, ldy, lddx)
 
 
 def sn_causal_conv1d_fwd(x, w, bias, y, offsets=None, seqs=1, state_in=None, state_out=None, silu=True):
-    xp, wp, yp, _, s = _conv1d_shape(x, w, y, "y", seqs, silu)
-    state = (seqs, s.width - 1, s.channels)
-    _call("sn_causal_conv1d_fwd", xp, wp, _dense(bias, (s.channels,), torch.float32, "bias"), yp, ctypes.byref(s), _offsets(offsets, seqs),
-          _dense(state_in, state, x.dtype, "state_in"), _dense(state_out, state, x.dtype, "state_out"), _stream())
+    device, xp, wp, yp, _, s = _conv1d_shape(x, w, y, "y", seqs, silu)
+    state, t = (seqs, w.shape[1] - 1, w.shape[0]), x.dtype
+    _call("sn_causal_conv1d_fwd", xp, wp, _dense(bias, state[2:], _f32, "bias", device), yp, s, _dense(offsets, (seqs + 1,), _int32, "offsets", device),
+          _dense(state_in, state, t, "state_in", device), _dense(state_out, state, t, "state_out", device), _stream_of(device))
 
 
 def sn_causal_conv1d_scratch_bytes(rows, channels, width):
@@ -138,46 +150,55 @@ def sn_causal_conv1d_scratch_bytes(rows, channels, width):
 
 
 def sn_causal_conv1d_bwd(x, w, bias, dy, dx, dw, dbias, scratch, offsets=None, seqs=1, state_in=None, dstate_out=None, dstate_in=None, silu=True):
-    xp, wp, gp, dxp, s = _conv1d_shape(x, w, dy, "dy", seqs, silu, dx)
-    state, vec = (seqs, s.width - 1, s.channels), (s.channels,)
-    sp, sb = _bytes(scratch, "scratch")
-    _call("sn_causal_conv1d_bwd", xp, wp, _dense(bias, vec, torch.float32, "bias"), gp, dxp, _dense(dw, (s.channels, s.width), torch.float32, "dw"),
-          _dense(dbias, vec, torch.float32, "dbias"), ctypes.byref(s), _offsets(offsets, seqs), _dense(state_in, state, x.dtype, "state_in"),
-          _dense(dstate_out, state, x.dtype, "dstate_out"), _dense(dstate_in, state, x.dtype, "dstate_in"), sp, sb, _stream())
+    device, xp, wp, gp, dxp, s = _conv1d_shape(x, w, dy, "dy", seqs, silu, dx)
+    state, t = (seqs, w.shape[1] - 1, w.shape[0]), x.dtype
+    sp, sb = _bytes(scratch, "scratch", device)
+    _call("sn_causal_conv1d_bwd", xp, wp, _dense(bias, state[2:], _f32, "bias", device), gp, dxp, _dense(dw, w.shape, _f32, "dw", device),
+          _dense(dbias, state[2:], _f32, "dbias", device), s, _dense(offsets, (seqs + 1,), _int32, "offsets", device),
+          _dense(state_in, state, t, "state_in", device), _dense(dstate_out, state, t, "dstate_out", device), _dense(dstate_in, state, t, "dstate_in", device),
+          sp, sb, _stream_of(device))
 
 
 def sn_causal_conv1d_step(x, w, bias, y, state, state_out=None, slots=None, silu=True):
     """One token for each row of x; state: (num_slots, width - 1, channels), updated in place unless state_out is given."""
-    xp, wp, yp, _, s = _conv1d_shape(x, w, y, "y", 1, silu)
-    shape = (state.shape[0], s.width - 1, s.channels)
-    sp = _dense(state, shape, x.dtype, "state")
-    _call("sn_causal_conv1d_step", xp, wp, _dense(bias, (s.channels,), torch.float32, "bias"), yp, sp,
-          sp if state_out is None else _dense(state_out, shape, x.dtype, "state_out"), _slots(slots, s.rows), shape[0], ctypes.byref(s), _stream())
+    device, xp, wp, yp, _, s = _conv1d_shape(x, w, y, "y", 1, silu)
+    shape, t = (state.shape[0], w.shape[1] - 1, w.shape[0]), x.dtype
+    sp = _dense(state, shape, t, "state", device)
+    _call("sn_causal_conv1d_step", xp, wp, _dense(bias, shape[2:], _f32, "bias", device), yp, sp,
+          sp if state_out is None else _dense(state_out, shape, t, "state_out", device), _dense(slots, x.shape[:1], _int32, "slots", device), shape[0], s,
+          _stream_of(device))
 
 
 # ---- norm of heads and position rotation ----
 def _headnorm_shape(q, k, yq, yk, inv_freq, head_dim, eps, interleaved, dq=None, dk=None):
+    if q.dim() != 2 or (k is not None and k.dim() != 2):
+        raise ValueError("q and k have to be (rows, heads * head_dim)")
     rows, nq = q.shape
     nk = k.shape[1] if k is not None else 0
     if head_dim < 1 or nq % head_dim or nk % head_dim:
         raise ValueError("the rows of q and k have to hold whole heads of head_dim = %d" % head_dim)
-    none = (None, 0)
-    ptrs = [_rows(t, rows, n, q.dtype, what) if t is not None else none
-            for t, n, what in ((q, nq, "q"), (k, nk, "k"), (yq, nq, "yq"), (yk, nk, "yk"), (dq, nq, "dq"), (dk, nk, "dk"))]
+    device, t = _device(q, "q"), q.dtype
+    none, sq, sk = (None, 0), (rows, nq), (rows, nk)
+    qp, ldq = _rows(q, sq, t, "q", device)
+    yqp, ldyq = _rows(yq, sq, t, "yq", device)
+    kp, ldk = _rows(k, sk, t, "k", device) if k is not None else none
+    ykp, ldyk = _rows(yk, sk, t, "yk", device) if yk is not None else none
+    dqp, lddq = _rows(dq, sq, t, "dq", device) if dq is not None else none
+    dkp, lddk = _rows(dk, sk, t, "dk", device) if dk is not None else none
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    s = HeadnormShape(rows, nq // head_dim, nk // head_dim, head_dim, rot, int(bool(interleaved)), _dtype_code(q), eps, *(p[1] for p in ptrs))
-    return [p[0] for p in ptrs], s
+    s = HeadnormShape(rows, nq // head_dim, nk // head_dim, head_dim, rot, 1 if interleaved else 0, _dtype_code(q), eps, ldq, ldk, ldyq, ldyk, lddq, lddk)
+    return device, qp, kp, yqp, ykp, dqp, dkp, s
 
 
-def _headnorm_args(wq, wk, positions, inv_freq, s):
-    return (_dense(wq, (s.head_dim,), torch.float32, "wq"), _dense(wk, (s.head_dim,), torch.float32, "wk"),
-            _dense(positions, (s.rows,), torch.int32, "positions"), _dense(inv_freq, (s.rot_dim // 2,), torch.float32, "inv_freq"))
+def _headnorm_args(wq, wk, positions, inv_freq, q, head_dim, device):
+    return (_dense(wq, (head_dim,), _f32, "wq", device), _dense(wk, (head_dim,), _f32, "wk", device), _dense(positions, q.shape[:1], _int32, "positions", device),
+            None if inv_freq is None else _dense(inv_freq, (inv_freq.numel(),), _f32, "inv_freq", device))
 
 
 def sn_headnorm_rot_fwd(q, k, wq, wk, positions, inv_freq, yq, yk, head_dim, eps=1e-6, interleaved=False):
     """q, k: (rows, heads * head_dim); k and yk may be None.  inv_freq has rot_dim / 2 elements, or is None for no rotation."""
-    (qp, kp, yqp, ykp, _, _), s = _headnorm_shape(q, k, yq, yk, inv_freq, head_dim, eps, interleaved)
-    _call("sn_headnorm_rot_fwd", qp, kp, *_headnorm_args(wq, wk, positions, inv_freq, s), yqp, ykp, ctypes.byref(s), _stream())
+    device, qp, kp, yqp, ykp, _, _, s = _headnorm_shape(q, k, yq, yk, inv_freq, head_dim, eps, interleaved)
+    _call("sn_headnorm_rot_fwd", qp, kp, *_headnorm_args(wq, wk, positions, inv_freq, q, head_dim, device), yqp, ykp, s, _stream_of(device))
 
 
 def sn_headnorm_rot_scratch_bytes(rows, q_heads, k_heads, head_dim):
@@ -185,11 +206,11 @@ def sn_headnorm_rot_scratch_bytes(rows, q_heads, k_heads, head_dim):
 
 
 def sn_headnorm_rot_bwd(q, k, wq, wk, positions, inv_freq, dyq, dyk, dq, dk, dwq, dwk, scratch, head_dim, eps=1e-6, interleaved=False):
-    (qp, kp, gqp, gkp, dqp, dkp), s = _headnorm_shape(q, k, dyq, dyk, inv_freq, head_dim, eps, interleaved, dq, dk)
+    device, qp, kp, gqp, gkp, dqp, dkp, s = _headnorm_shape(q, k, dyq, dyk, inv_freq, head_dim, eps, interleaved, dq, dk)
     vec = (head_dim,)
-    sp, sb = _bytes(scratch, "scratch")
-    _call("sn_headnorm_rot_bwd", qp, kp, *_headnorm_args(wq, wk, positions, inv_freq, s), gqp, gkp, dqp, dkp,
-          _dense(dwq, vec, torch.float32, "dwq"), _dense(dwk, vec, torch.float32, "dwk"), ctypes.byref(s), sp, sb, _stream())
+    sp, sb = _bytes(scratch, "scratch", device)
+    _call("sn_headnorm_rot_bwd", qp, kp, *_headnorm_args(wq, wk, positions, inv_freq, q, head_dim, device), gqp, gkp, dqp, dkp,
+          _dense(dwq, vec, _f32, "dwq", device), _dense(dwk, vec, _f32, "dwk", device), s, sp, sb, _stream_of(device))
 
 
 # ---- selective state space scan ----
@@ -210,22 +231,28 @@ def sn_scan_states_bytes(shape):
 
 
 def _scan_inputs(u, dt, A, B, C, D, z, dt_bias, y, what, seqs, softplus, ragged):
-    rows, channels = u.shape
+    if u.dim() != 2 or A.dim() != 2:
+        raise ValueError("u has to be (rows, channels), A (channels, states)")
+    shape = u.shape
+    rows, channels = shape
     states = A.shape[1]
     if states < 1 or B.dim() != 2 or B.shape[1] % states:
         raise ValueError("the rows of B and C have to hold whole groups of states = %d" % states)
-    t, vec, gn = u.dtype, (channels,), B.shape[1]
-    ptrs = [_rows(v, rows, n, t, name) for v, n, name in ((u, channels, "u"), (dt, channels, "dt"), (B, gn, "B"), (C, gn, "C"))]
-    ptrs.append(_rows(z, rows, channels, t, "z") if z is not None else (None, 0))
-    ptrs.append(_rows(y, rows, channels, t, what))
-    s = ScanShape(rows, seqs, channels, states, gn // states, _dtype_code(u), int(bool(softplus)), int(ragged), *(p[1] for p in ptrs))
-    up, dtp, bp, cp, zp, yp = (p[0] for p in ptrs)
-    return s, (up, dtp, _dense(A, (channels, states), torch.float32, "A"), bp, cp, _dense(D, vec, torch.float32, "D"), zp,
-               _dense(dt_bias, vec, torch.float32, "dt_bias"), yp)
+    device, t = _device(u, "u"), u.dtype
+    vec, bc = (channels,), (rows, B.shape[1])
+    up, ldu = _rows(u, shape, t, "u", device)
+    dtp, lddt = _rows(dt, shape, t, "dt", device)
+    bp, ldb = _rows(B, bc, t, "B", device)
+    cp, ldc = _rows(C, bc, t, "C", device)
+    zp, ldz = _rows(z, shape, t, "z", device) if z is not None else (None, 0)
+    yp, ldy = _rows(y, shape, t, what, device)
+    s = ScanShape(rows, seqs, channels, states, bc[1] // states, _dtype_code(u), 1 if softplus else 0, 1 if ragged else 0, ldu, lddt, ldb, ldc, ldz, ldy)
+    return device, s, (up, dtp, _dense(A, (channels, states), _f32, "A", device), bp, cp, _dense(D, vec, _f32, "D", device), zp,
+                       _dense(dt_bias, vec, _f32, "dt_bias", device), yp)
 
 
-def _states(states, s):
-    p, n = _bytes(states, "states")
+def _states(states, s, device):
+    p, n = _bytes(states, "states", device)
     if states is not None and n < sn_scan_states_bytes(s):
         raise ValueError("states: %d bytes, needs %d" % (n, sn_scan_states_bytes(s)))
     return p
@@ -233,32 +260,32 @@ def _states(states, s):
 
 def sn_scan_fwd(u, dt, A, B, C, D, z, dt_bias, y, offsets=None, seqs=1, h0=None, hT=None, states=None, workspace=None, softplus=True):
     """u, dt, z, y: (rows, channels); A: (channels, states); B, C: (rows, groups * states); D, z, dt_bias may be None."""
-    s, args = _scan_inputs(u, dt, A, B, C, D, z, dt_bias, y, "y", seqs, softplus, offsets is not None)
-    h = (seqs, s.channels, s.states)
-    wp, wb = _bytes(workspace, "workspace")
-    _call("sn_scan_fwd", *args, ctypes.byref(s), _offsets(offsets, seqs), _dense(h0, h, torch.float32, "h0"), _dense(hT, h, torch.float32, "hT"),
-          _states(states, s), wp, wb, _stream())
+    device, s, args = _scan_inputs(u, dt, A, B, C, D, z, dt_bias, y, "y", seqs, softplus, offsets is not None)
+    h = (seqs, *A.shape)
+    wp, wb = _bytes(workspace, "workspace", device)
+    _call("sn_scan_fwd", *args, s, _dense(offsets, (seqs + 1,), _int32, "offsets", device), _dense(h0, h, _f32, "h0", device), _dense(hT, h, _f32, "hT", device),
+          _states(states, s, device), wp, wb, _stream_of(device))
 
 
 def sn_scan_bwd(u, dt, A, B, C, D, z, dt_bias, dy, du, ddt, dA, dB, dC, dD, dz, ddt_bias, workspace, offsets=None, seqs=1, h0=None, states=None,
                 dhT=None, dh0=None, softplus=True):
-    s, args = _scan_inputs(u, dt, A, B, C, D, z, dt_bias, dy, "dy", seqs, softplus, offsets is not None)
-    t, gn, vec, h = u.dtype, s.groups * s.states, (s.channels,), (seqs, s.channels, s.states)
-    dup, s.ld_du = _rows(du, s.rows, s.channels, t, "du")
-    ddtp, s.ld_ddt = _rows(ddt, s.rows, s.channels, t, "ddt")
-    dbp, s.ld_db = _rows(dB, s.rows, gn, t, "dB")
-    dcp, s.ld_dc = _rows(dC, s.rows, gn, t, "dC")
-    dzp, s.ld_dz = _rows(dz, s.rows, s.channels, t, "dz") if dz is not None else (None, 0)
-    wp, wb = _bytes(workspace, "workspace")
-    _call("sn_scan_bwd", *args, dup, ddtp, _dense(dA, (s.channels, s.states), torch.float32, "dA"), dbp, dcp, _dense(dD, vec, torch.float32, "dD"), dzp,
-          _dense(ddt_bias, vec, torch.float32, "ddt_bias"), ctypes.byref(s), _offsets(offsets, seqs), _dense(h0, h, torch.float32, "h0"), _states(states, s),
-          _dense(dhT, h, torch.float32, "dhT"), _dense(dh0, h, torch.float32, "dh0"), wp, wb, _stream())
+    device, s, args = _scan_inputs(u, dt, A, B, C, D, z, dt_bias, dy, "dy", seqs, softplus, offsets is not None)
+    t, shape, bc, vec, h = u.dtype, u.shape, B.shape, u.shape[1:], (seqs, *A.shape)
+    dup, s.ld_du = _rows(du, shape, t, "du", device)
+    ddtp, s.ld_ddt = _rows(ddt, shape, t, "ddt", device)
+    dbp, s.ld_db = _rows(dB, bc, t, "dB", device)
+    dcp, s.ld_dc = _rows(dC, bc, t, "dC", device)
+    dzp, s.ld_dz = _rows(dz, shape, t, "dz", device) if dz is not None else (None, 0)
+    wp, wb = _bytes(workspace, "workspace", device)
+    _call("sn_scan_bwd", *args, dup, ddtp, _dense(dA, A.shape, _f32, "dA", device), dbp, dcp, _dense(dD, vec, _f32, "dD", device), dzp,
+          _dense(ddt_bias, vec, _f32, "ddt_bias", device), s, _dense(offsets, (seqs + 1,), _int32, "offsets", device), _dense(h0, h, _f32, "h0", device),
+          _states(states, s, device), _dense(dhT, h, _f32, "dhT", device), _dense(dh0, h, _f32, "dh0", device), wp, wb, _stream_of(device))
 
 
 def sn_scan_step(u, dt, A, B, C, D, z, dt_bias, y, state, state_out=None, slots=None, softplus=True):
     """One token for each row of u; state: fp32 (num_slots, channels, states), updated in place unless state_out is given."""
-    s, args = _scan_inputs(u, dt, A, B, C, D, z, dt_bias, y, "y", 1, softplus, False)
-    shape = (state.shape[0], s.channels, s.states)
-    sp = _dense(state, shape, torch.float32, "state")
-    _call("sn_scan_step", *args, sp, sp if state_out is None else _dense(state_out, shape, torch.float32, "state_out"), _slots(slots, s.rows), shape[0],
-          ctypes.byref(s), _stream())
+    device, s, args = _scan_inputs(u, dt, A, B, C, D, z, dt_bias, y, "y", 1, softplus, False)
+    shape = (state.shape[0], *A.shape)
+    sp = _dense(state, shape, _f32, "state", device)
+    _call("sn_scan_step", *args, sp, sp if state_out is None else _dense(state_out, shape, _f32, "state_out", device),
+          _dense(slots, u.shape[:1], _int32, "slots", device), shape[0], s, _stream_of(device))

@@ -167,7 +167,7 @@ def test_scan_refusals_of_one_call():
 
 
 def test_scan_workspace_grows_with_the_tokens_where_channels_are_few():
-    wide, narrow = sn.scan_shape(8 * 2048, 4096, 16, seqs=8), sn.scan_shape(32768, 64, 16)
+    wide, narrow = sn.scan_shape(32 * 512, 4096, 16, seqs=32), sn.scan_shape(32768, 64, 16)
     assert sn.sn_scan_workspace_query(wide, sn.SN_SCAN_FWD) == (0, 0)
     assert sn.sn_scan_workspace_query(narrow, sn.SN_SCAN_FWD)[1] > 0
     # the state before every 16th token
