@@ -204,24 +204,36 @@ template <typename T, int NL, bool WHOLE> struct Staged {
     __device__ void set(int i, float v) { p[i / P].set(i % P, v); }
 };
 
-// A row's B or C of one group: NP values, a thread's share of a tile, of which the first `rows` are in the tensor.
-template <typename T, int NL, int ROWS> struct StagedBC {
-    static constexpr int NP = ScanGeo<NL>::NP, COUNT = ROWS * NP, PER = (COUNT + 255) / 256;
-    T v[PER];
-    __device__ void load(const char *tile, uint32_t ld, int rows, int N)
+// The rows of B and C of one group, NP values each, a thread's share of a tile of which the first `have` rows are in the tensors.  WHOLE: four
+// neighbouring states at a time, so that a wave or two load what all four would one by one.  first .. last - 1: the rows of the piece, the
+// others are staged as zeros.
+template <typename T, int NL, int ROWS, bool BOTH, bool WHOLE> struct StagedBC {
+    static constexpr int NP = ScanGeo<NL>::NP, V = WHOLE ? 4 : 1, EACH = ROWS * NP / V, COUNT = (BOTH ? 2 : 1) * EACH, PER = (COUNT + 255) / 256;
+    Pack<T, V> v[PER];
+    // B, C: the tile's first rows; the first alone unless BOTH
+    __device__ void load(const char *B, uint32_t ld_b, const char *C, uint32_t ld_c, int have, int N)
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int k = i * 256 + threadIdx.x;
-            v[i] = *reinterpret_cast<const T *>(tile + (uint32_t)(min(k / NP % ROWS, rows - 1) * ld + min(k % NP, N - 1) * (uint32_t)sizeof(T)));
+            const int k = i * 256 + threadIdx.x, r = min(k % EACH * V / NP, have - 1), n = k * V % NP;
+            const uint32_t at = (uint32_t)(WHOLE ? (n < N ? n : 0) : min(n, N - 1)) * (uint32_t)sizeof(T);
+            v[i].load(reinterpret_cast<const T *>(BOTH && k / EACH % 2 ? C + (uint32_t)(r * ld_c + at) : B + (uint32_t)(r * ld_b + at)));
         }
     }
-    __device__ void put(float *lds, int first, int last, int N) const   // rows first .. last - 1 of the tile, zeros around them
+    __device__ void put(float *s_B, float *s_C, int first, int last, int N) const
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int k = i * 256 + threadIdx.x, r = k / NP;
-            if (k < COUNT) lds[k] = k % NP < N && r >= first && r < last ? seq_ld<T>(&v[i]) : 0.f;
+            const int k = i * 256 + threadIdx.x, w = k % EACH, r = w * V / NP, n = k * V % NP;
+            if (k >= COUNT) continue;
+            float *to = (BOTH && k >= EACH ? s_C : s_B) + w * V;
+            const bool here = r >= first && r < last;
+            if (WHOLE) {
+                const bool in = here && n < N;
+                *reinterpret_cast<float4 *>(to) = make_float4(keep_if(in, v[i].get(0)), keep_if(in, v[i].get(V > 1 ? 1 : 0)), keep_if(in, v[i].get(V > 1 ? 2 : 0)), keep_if(in, v[i].get(V > 1 ? 3 : 0)));
+            } else {
+                to[0] = keep_if(here && n < N, v[i].get(0));
+            }
         }
     }
 };
@@ -238,6 +250,7 @@ size_t scan_carry_bytes(const sn_scan_shape &s, const ScanPlan &p);
 ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off, const void *u, const void *dt, const float *A, const void *B, const void *C,
                    const float *D, const void *z, const float *bias);
 bool scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan);
+bool scan_whole_states(const void *p, int64_t ld, const sn_scan_shape &s);
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws);
 hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st);   // a.states from the inputs
 hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st);

@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
         SeqAt at = seq_find(a.rows, r0);
         Piece next = piece_from<ROWS>(a.rows, at, r0, r0, r1);
         Staged<T, NL, WHOLE> u[RP], dt[RP], z[RP];
-        StagedBC<T, NL, ROWS> B, C;
+        StagedBC<T, NL, ROWS, OUT, WHOLE> BC;
         const auto fetch = [&]() {
             const int64_t t0 = next.t0;
             const int have = a.rows.rows - next.t0;   // rows of the tensors from there on
@@ -65,8 +65,7 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
                 dt[j].load(pdt + t0 * a.ld_dt, a.ld_dt, r, co, nch);
                 if (OUT) z[j].load(pz + t0 * a.ld_z, a.ld_z, r, co, nch);
             }
-            B.load(pB + t0 * a.ld_b, a.ld_b, have, a.N);
-            if (OUT) C.load(pC + t0 * a.ld_c, a.ld_c, have, a.N);
+            BC.load(pB + t0 * a.ld_b, a.ld_b, pC + t0 * a.ld_c, a.ld_c, have, a.N);
         };
         float uu[RP][VE], gate[RP][VE];
         const auto stage = [&](const Piece &p) {
@@ -85,8 +84,7 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
                     if (OUT) gate[j][i] = pick(is_gate, z[j].get(i) * sigmoid(z[j].get(i)), 1.f);
                 }
             }
-            B.put(s_B, first, last, a.N);
-            if (OUT) C.put(s_C, first, last, a.N);
+            BC.put(s_B, s_C, first, last, a.N);
         };
         Piece now = next;
         if (now.any) {
@@ -204,8 +202,9 @@ __global__ void __launch_bounds__(THREADS) scan_carry_kernel(ScanArgs a, int rev
     }
 }
 
-// One token: a thread holds four states of a channel, NL neighbouring threads a channel.
-template <typename T, int NL>
+// One token: a thread holds four states of a channel, NL neighbouring threads a channel.  Bound by reading and writing the states.  WHOLE: a
+// thread's four are there and aligned, in the states, in A and in the rows of B and C.
+template <typename T, int NL, bool WHOLE>
 __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const float *state, float *state_out, const int32_t *slots, int num_slots)
 {
     const int slot = step_slot(slots, blockIdx.x, num_slots);
@@ -214,29 +213,50 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     const int k = blockIdx.y * THREADS + threadIdx.x, c = k / NL, n0 = k % NL * 4;
     if (c >= a.channels) return;
     const int group = c / a.per_group;
-    const float u = seq_ld<T>((const T *)((const char *)a.u + t * a.ld_u) + c);
+    const float *from = state + ((int64_t)slot * a.channels + c) * a.N, *A = a.A + (int64_t)c * a.N;
+    float *to = state_out + ((int64_t)slot * a.channels + c) * a.N;
+    const T *B = (const T *)((const char *)a.B + t * a.ld_b) + group * a.N, *C = (const T *)((const char *)a.C + t * a.ld_c) + group * a.N;
+    float h[4], A4[4];
+    Pack<T, 4> b, cc;
+    if (WHOLE) {
+        const int n = n0 < a.N ? n0 : 0;
+        *reinterpret_cast<float4 *>(h) = *reinterpret_cast<const float4 *>(from + n);
+        *reinterpret_cast<float4 *>(A4) = *reinterpret_cast<const float4 *>(A + n);
+        b.load(B + n);
+        cc.load(C + n);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = min(n0 + i, a.N - 1);
+            h[i] = from[n];
+            A4[i] = A[n];
+            b.e[i] = B[n];
+            cc.e[i] = C[n];
+        }
+    }
+    const float u = seq_ld<T>((const T *)((const char *)a.u + t * a.ld_u) + c), z = seq_ld<T>((const T *)((const char *)a.z + t * a.ld_z) + c);
     float raw = seq_ld<T>((const T *)((const char *)a.dt + t * a.ld_dt) + c);
     if (a.bias) raw += a.bias[c];
+    const float skip = a.D ? a.D[c] : 0.f;
     const float delta = a.softplus ? softplus(raw) : raw;
-    const T *B = (const T *)((const char *)a.B + t * a.ld_b) + group * a.N + n0, *C = (const T *)((const char *)a.C + t * a.ld_c) + group * a.N + n0;
-    const float *from = state + ((int64_t)slot * a.channels + c) * a.N + n0, *A = a.A + (int64_t)c * a.N + n0;
-    float *to = state_out + ((int64_t)slot * a.channels + c) * a.N + n0;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (n0 + i >= a.N) continue;
-        const float h = fmaf(exp_fast(delta * A[i]), from[i], delta * u * seq_ld<T>(B + i));
-        sum = fmaf(h, seq_ld<T>(C + i), sum);
-        to[i] = h;
+        h[i] = fmaf(exp_fast(delta * A4[i]), h[i], delta * u * b.get(i));
+        if (n0 + i < a.N) sum = fmaf(h[i], cc.get(i), sum);
+    }
+    if (WHOLE) {
+        if (n0 < a.N) *reinterpret_cast<float4 *>(to + n0) = make_float4(h[0], h[1], h[2], h[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n0 + i < a.N) to[n0 + i] = h[i];
     }
 #pragma unroll
     for (int m = NL / 2; m >= 1; m /= 2) sum += __shfl_xor(sum, m, 64);
     if (n0) return;
-    float y = a.D ? fmaf(a.D[c], u, sum) : sum;
-    if (a.gate) {
-        const float z = seq_ld<T>((const T *)((const char *)a.z + t * a.ld_z) + c);
-        y *= z * sigmoid(z);
-    }
+    float y = fmaf(skip, u, sum);
+    if (a.gate) y *= z * sigmoid(z);
     seq_st((T *)((char *)a.y + t * a.ld_y) + c, y);
 }
 
@@ -317,6 +337,12 @@ bool scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const Sc
     return rows_aligned(p, s.rows > 1 ? ld : 0, e, piece) && s.channels / s.groups % ve == 0;
 }
 
+// Whether the rows of B or C can be staged four states at a time.
+bool scan_whole_states(const void *p, int64_t ld, const sn_scan_shape &s)
+{
+    return s.states % 4 == 0 && rows_aligned(p, s.rows > 1 ? ld : 0, s.dtype == SN_BF16 ? 2 : 4, 4);
+}
+
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws)
 {
     char *at = (char *)ws;
@@ -361,7 +387,7 @@ hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const 
     ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
     a.y = y; a.h0 = h0; a.hT = hT; a.states = states;
     const bool whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && scan_whole_rows(y, s.ld_y, s, p) &&
-                       (!z || scan_whole_rows(z, s.ld_z, s, p));
+                       (!z || scan_whole_rows(z, s.ld_z, s, p)) && scan_whole_states(B, s.ld_b, s) && scan_whole_states(C, s.ld_c, s);
     if (p.parts > 1) scan_set_carry(a, s, p, ws);
     return fwd_in_chunks<0>(a, s, p, whole, st);
 }
@@ -373,9 +399,17 @@ hipError_t launch_scan_step(const void *u, const void *dt, const float *A, const
     ScanArgs a = scan_args(s, p, nullptr, u, dt, A, B, C, D, z, bias);
     a.y = y;
     const dim3 grid((int)s.rows, div_up((int64_t)s.channels * p.NL, THREADS));
+    const int e = s.dtype == SN_BF16 ? 2 : 4;
+    const bool whole = s.states % 4 == 0 && rows_aligned(state, 0, 4, 4) && rows_aligned(state_out, 0, 4, 4) && rows_aligned(A, 0, 4, 4) &&
+                       rows_aligned(B, s.rows > 1 ? s.ld_b : 0, e, 4) && rows_aligned(C, s.rows > 1 ? s.ld_c : 0, e, 4);
     return by_lanes(p.NL, [&](auto NL) {
-        if (s.dtype == SN_BF16) scan_step_kernel<bf16_t, NL.value><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
-        else scan_step_kernel<float, NL.value><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+        if (s.dtype == SN_BF16) {
+            if (whole) scan_step_kernel<bf16_t, NL.value, true><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+            else scan_step_kernel<bf16_t, NL.value, false><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+        } else {
+            if (whole) scan_step_kernel<float, NL.value, true><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+            else scan_step_kernel<float, NL.value, false><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);
+        }
         return hipGetLastError();
     });
 }

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     SeqAt at = seq_find(a.rows, r1 - 1);
     Piece next = piece_before<TS>(a.rows, at, r1, r0);
     Staged<T, NL, WHOLE> dt, z, dy;
-    StagedBC<T, NL, TS> C;
+    StagedBC<T, NL, TS, false, WHOLE> C;
     const char *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T), *pdy = (const char *)a.dy + c0 * sizeof(T);
     const char *pC = (const char *)a.C + group * a.N * sizeof(T);
     const uint32_t is_softplus = a.softplus ? ~0u : 0u, is_gate = a.gate ? ~0u : 0u;
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
         dt.load(pdt + t0 * a.ld_dt, a.ld_dt, r, co, nch);
         dy.load(pdy + t0 * a.ld_y, a.ld_y, r, co, nch);
         z.load(pz + t0 * a.ld_z, a.ld_z, r, co, nch);
-        C.load(pC + t0 * a.ld_c, a.ld_c, have, a.N);
+        C.load(pC + t0 * a.ld_c, a.ld_c, nullptr, 0, have, a.N);
     };
     const auto stage = [&](const Piece &p) {
         const int first = p.p0 - p.t0, last = p.p1 - p.t0;
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
             s_delta[row][co + i] = keep_if(here, pick(is_softplus, softplus(raw), raw));
             s_g[row][co + i] = keep_if(here, dy.get(i) * pick(is_gate, z.get(i) * sigmoid(z.get(i)), 1.f));
         }
-        C.put(s_C, first, last, a.N);
+        C.put(s_C, nullptr, first, last, a.N);
     };
     Piece now = next;
     if (now.any) {
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
     constexpr int CB = G::CB, NP = G::NP, VE = G::VE, CW = G::CW;
     __shared__ float s_delta[TS][CB], s_x[TS][CB], s_g[TS][CB], s_y[TS][CB], s_qa[TS][CB], s_dD[TS][CB], s_dbias[TS][CB], s_bias[CB], s_skip[CB];
     __shared__ alignas(16) float s_B[TS * NP], s_C[TS * NP];
-    __shared__ float s_bc[4][TS][2 * NP];
+    __shared__ alignas(16) float s_bc[4][TS][2 * NP];
 
     const int chunk = blockIdx.x, span = chunk / a.parts, part = chunk % a.parts;
     const int group = blockIdx.y / a.blocks_per_group, inside = blockIdx.y % a.blocks_per_group * CB;
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
         SeqAt at = seq_find(a.rows, r1 - 1);
         Piece next = piece_before<TS>(a.rows, at, r1, r0);
         Staged<T, NL, WHOLE> u, dt, z, dy;
-        StagedBC<T, NL, TS> B, C;
+        StagedBC<T, NL, TS, true, WHOLE> BC;
         float4 kept = {};   // the state in front of the piece's tile
         const auto fetch = [&]() {
             const int64_t t0 = next.t0;
@@ -166,8 +166,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
             dt.load(pdt + t0 * a.ld_dt, a.ld_dt, r, co, nch);
             dy.load(pdy + t0 * a.ld_y, a.ld_y, r, co, nch);
             z.load(pz + t0 * a.ld_z, a.ld_z, r, co, nch);
-            B.load(pB + t0 * a.ld_b, a.ld_b, have, a.N);
-            C.load(pC + t0 * a.ld_c, a.ld_c, have, a.N);
+            BC.load(pB + t0 * a.ld_b, a.ld_b, pC + t0 * a.ld_c, a.ld_c, have, a.N);
             kept = lane.fetch_own(a.states, (int64_t)span * a.tiles_per_span + (next.t0 - span * a.span_rows) / TS, a);
         };
         // Of the staged piece, what its gradients take besides what is in LDS: u, d delta / d dt, d y / d z without y.  Made here, not kept as
@@ -189,8 +188,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                 s_x[row][co + i] = delta * uu[i];
                 s_g[row][co + i] = keep_if(here, pick(is_gate, d * (zz * sz), d));
             }
-            B.put(s_B, begin, last, a.N);
-            C.put(s_C, begin, last, a.N);
+            BC.put(s_B, s_C, begin, last, a.N);
             lane.take(kept, a, first);
             if (p.start) {
                 if (a.h0) lane.load(a.h0, p.seq, a, first);
@@ -243,19 +241,9 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                     float hs[HR + 1][4], decay[HR][4];   // hs[k]: the state in front of the half's row k
 #pragma unroll
                     for (int i = 0; i < 4; ++i) hs[0][i] = half ? mid[i] : first[i];
-                    // the states, forwards
+                    // the states, forwards; rows that are not the piece's leave them as they are
 #pragma unroll
                     for (int kb = 0; kb < HR; kb += GR) {
-                        if (outside(half + kb, GR)) {
-#pragma unroll
-                            for (int k = kb; k < kb + GR; ++k)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    hs[k + 1][i] = hs[k][i];
-                                    decay[k][i] = 1.f;
-                                }
-                            continue;
-                        }
                         float acc[NL];
                         RowIn r, ahead = read(half + kb);
 #pragma unroll
@@ -335,12 +323,14 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
                 s_dbias[row][co + i] += keep_if(here, dd);
                 s_dD[row][co + i] = fmaf(gy, uu[i], s_dD[row][co + i]);   // both are zero elsewhere
             }
-            constexpr int PER = (TS * 2 * NP + THREADS - 1) / THREADS;
-            float bc[PER];
+            constexpr int PER = (TS * 2 * NP / 4 + THREADS - 1) / THREADS;
+            float4 bc[PER];
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int k = i * THREADS + threadIdx.x, r = k / (2 * NP) % TS, n = k % (2 * NP);
-                bc[i] = s_bc[0][r][n] + s_bc[1][r][n] + s_bc[2][r][n] + s_bc[3][r][n];
+                const int k = i * THREADS + threadIdx.x, r = k * 4 / (2 * NP) % TS, n = k * 4 % (2 * NP);
+                const auto at = [&](int w) { return *reinterpret_cast<const float4 *>(&s_bc[w][r][n]); };
+                const float4 p = at(0), q = at(1), v = at(2), w = at(3);
+                bc[i] = make_float4(p.x + q.x + v.x + w.x, p.y + q.y + v.y + w.y, p.z + q.z + v.z + w.z, p.w + q.w + v.w + w.w);
             }
             // The next rows are staged before anything is stored: whoever waits for the loads waits for what was stored since as well.
             if (next.any) stage(next);
@@ -351,8 +341,8 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
             }
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const uint32_t k = i * THREADS + threadIdx.x, r = k / (2 * NP);
-                if (r < TS && now.holds(now.t0 + r)) (part_bc + (int64_t)now.t0 * (2 * NP))[k] = bc[i];
+                const uint32_t k = i * THREADS + threadIdx.x, r = k * 4 / (2 * NP);
+                if (r < TS && now.holds(now.t0 + r)) *reinterpret_cast<float4 *>(part_bc + (int64_t)now.t0 * (2 * NP) + k * 4) = bc[i];
             }
             now = next;
             if (now.any) {
@@ -461,7 +451,8 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
     a.h0 = h0;
     a.dy = g.dy; a.du = g.du; a.ddt = g.ddt; a.dB = g.dB; a.dC = g.dC; a.dz = g.dz; a.dhT = g.dhT; a.dh0 = g.dh0;
-    const bool in_whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && (!z || scan_whole_rows(z, s.ld_z, s, p));
+    const bool in_whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && (!z || scan_whole_rows(z, s.ld_z, s, p)) &&
+                          scan_whole_states(B, s.ld_b, s) && scan_whole_states(C, s.ld_c, s);
     const bool whole = in_whole && scan_whole_rows(g.dy, s.ld_y, s, p) && scan_whole_rows(g.du, s.ld_du, s, p) && scan_whole_rows(g.ddt, s.ld_ddt, s, p) &&
                        (!z || scan_whole_rows(g.dz, s.ld_dz, s, p));
     char *at = (char *)ws;
