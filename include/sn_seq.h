@@ -13,7 +13,8 @@
  *    seq_offsets[s] .. seq_offsets[s+1] - 1.  Empty sequences are allowed.  Rows that no sequence holds (behind the last) are
  *    neither read for any result nor written.  Offsets that descend, or leave 0 .. rows, give undefined results, but no access
  *    outside the tensors.
- *  - rows and every product of sizes without rows fit int32; addresses are 64-bit.  rows = 0 is a valid call.
+ *  - Sizes, SN_ERR_UNSUPPORTED beyond: rows 2^30 (of a step call 2^24 - 1), sequences 2^24 - 1, channels of the convolution 65535 * 256,
+ *    channels of the scan 65535 blocks of 16 of one group.  Addresses are 64-bit.  rows = 0 is a valid call.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
  *  - Arithmetic, states and sums are fp32; a result of `dtype` is rounded once.  Sums are in a fixed order: results are
  *    run-to-run identical.
@@ -101,7 +102,7 @@ sn_status sn_headnorm_rot_bwd(const void *q, const void *k, const float *wq, con
  *   y = (sum_n C[t,g,n] * h[d,n] + D[d] * u) * (z ? z * sigmoid(z) : 1)
  * u, dt, z, y: rows x channels; B, C: rows x (groups * states); A: fp32 [channels][states]; D, dt_bias: fp32 [channels].  D, dt_bias
  * and z may be NULL.  h0, hT: fp32 [seqs][channels][states], the initial (NULL: zeros) and the final state; hT may be NULL, and must
- * not overlap h0.
+ * not overlap h0.  Row strides of the scan stay below 2^24 elements (SN_ERR_UNSUPPORTED).
  * Workspace and speed: a call needs parallel work beyond channels x sequences only where these are few; then it cuts the
  * tokens into chunks whose states are joined through the workspace.  With less than preferred_bytes it cuts into fewer chunks, with
  * the least into none; the result differs by the rounding of the joins only. */
@@ -124,8 +125,8 @@ typedef struct {
 sn_status sn_scan_workspace_query(const sn_scan_shape *shape, sn_scan_dir dir, size_t *min_bytes, size_t *preferred_bytes);
 
 /* What the backward pass needs of the forward pass: the state before every 16th token.  Kept (sn_scan_fwd's `states`) or left out and
- * replayed from the inputs by sn_scan_bwd (Sec. 3.4: recomputation), with the same results bit for bit where both calls are given the same
- * workspace. */
+ * replayed from the inputs by sn_scan_bwd (Sec. 3.4: recomputation); the results differ by the rounding of the joins only, as a replay may
+ * cut the tokens elsewhere.  256-byte aligned. */
 size_t sn_scan_states_bytes(const sn_scan_shape *shape);
 
 sn_status sn_scan_fwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z,

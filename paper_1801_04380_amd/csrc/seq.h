@@ -83,6 +83,16 @@ __device__ inline void seq_forward(const SeqRows &r, SeqAt &a, int row)
     }
 }
 
+// f(s) for the sequences without rows, by all lanes of a wave together: 64 offsets are looked at at a time.
+template <typename F> __device__ inline void each_empty(const SeqRows &r, F f)
+{
+    for (int s0 = 0; s0 < r.seqs; s0 += 64) {
+        const int s = s0 + (threadIdx.x & 63);
+        uint64_t empty = __ballot(s < r.seqs && (!r.off || r.off[s] == r.off[s + 1]));
+        for (; empty; empty &= empty - 1) f(s0 + __builtin_ctzll(empty));
+    }
+}
+
 // The instructions for 2^x, log2 x and 1 / x, each within one unit of the last place; e^x and log through them.  For |x| up to 20 the product with
 // log2(e) adds 20 * 2^-24 to the relative error of e^x.  2^x below 2^-126 is 0.
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -6,6 +6,9 @@ using namespace sn;
 namespace {
 
 constexpr int64_t INT32_MOST = 0x7fffffffLL;
+constexpr int64_t ROWS_MOST = 1 << 30;            // the kernels look a tile further in 32 bits
+constexpr int64_t GRID_MOST = (1 << 24) - 1;      // workgroups of 256 threads in a grid's first dimension: sequences, rows of a step
+constexpr int64_t GRID_Y_MOST = 65535;            // and in its second: blocks of channels
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 size_t esize(int dtype) { return dtype == SN_BF16 ? 2 : 4; }
@@ -30,18 +33,18 @@ sn_status check_rows(int64_t rows, int32_t seqs, bool ragged)
 {
     if (rows < 0 || seqs < 1) return SN_ERR_BAD_ARG;
     if (!ragged && rows % seqs) return SN_ERR_BAD_ARG;
-    if (rows > INT32_MOST || seqs >= INT32_MOST) return SN_ERR_UNSUPPORTED;
+    if (rows > ROWS_MOST || seqs > GRID_MOST) return SN_ERR_UNSUPPORTED;
     return SN_OK;
 }
 
 sn_status check_conv1d(const sn_conv1d_shape *s, const void *x, const void *w, const float *bias, const void *y)
 {
     if (!s || s->rows < 0 || s->channels < 1 || s->width < 1 || !valid_dtype(s->dtype) || !flag(s->silu)) return SN_ERR_BAD_ARG;
-    if (s->width > SN_CONV1D_MAX_WIDTH || s->rows > INT32_MOST) return SN_ERR_UNSUPPORTED;
+    if (s->width > SN_CONV1D_MAX_WIDTH || s->rows > ROWS_MOST) return SN_ERR_UNSUPPORTED;
     const size_t e = esize(s->dtype);
     if (!tensor(x, e, s->rows) || !tensor(y, e, s->rows) || !w || !aligned(w, e) || !optional(bias, 4) || same(x, y)) return SN_ERR_BAD_ARG;
     if (!stride(s->ld_x, s->channels, s->rows) || !stride(s->ld_y, s->channels, s->rows)) return SN_ERR_BAD_ARG;
-    if ((int64_t)s->channels * s->width > INT32_MOST) return SN_ERR_UNSUPPORTED;
+    if (s->channels > GRID_Y_MOST * 256) return SN_ERR_UNSUPPORTED;
     return SN_OK;
 }
 
@@ -51,7 +54,7 @@ sn_status check_slots(const void *state, const void *state_out, size_t align, co
     if (num_slots < 0 || (!none && rows && num_slots && (!state || !state_out)) || !aligned(state, align) || !aligned(state_out, align) || !aligned(slots, 4))
         return SN_ERR_BAD_ARG;
     if (!slots && rows > num_slots) return SN_ERR_BAD_ARG;
-    return SN_OK;
+    return rows > GRID_MOST ? SN_ERR_UNSUPPORTED : SN_OK;
 }
 
 sn_status check_headnorm(const sn_headnorm_shape *s, const void *q, const void *k, const float *wq, const float *wk, const int32_t *positions, const float *inv_freq,
@@ -60,7 +63,7 @@ sn_status check_headnorm(const sn_headnorm_shape *s, const void *q, const void *
     if (!s || s->rows < 0 || s->q_heads < 1 || s->k_heads < 0 || s->head_dim < 2 || s->head_dim % 2 || s->rot_dim < 0 || s->rot_dim % 2 || s->rot_dim > s->head_dim ||
         !flag(s->interleaved) || !valid_dtype(s->dtype) || !(s->eps > 0.f))
         return SN_ERR_BAD_ARG;
-    if (s->head_dim > SN_HEADNORM_MAX_DIM || s->rows > INT32_MOST || (int64_t)s->q_heads + s->k_heads > (1 << 20)) return SN_ERR_UNSUPPORTED;
+    if (s->head_dim > SN_HEADNORM_MAX_DIM || s->rows > ROWS_MOST || (int64_t)s->q_heads + s->k_heads > (1 << 20)) return SN_ERR_UNSUPPORTED;
     const size_t e = esize(s->dtype);
     const int64_t nq = (int64_t)s->q_heads * s->head_dim, nk = (int64_t)s->k_heads * s->head_dim;
     if (!tensor(q, e, s->rows) || !tensor(yq, e, s->rows) || !stride(s->ld_q, nq, s->rows) || !stride(s->ld_yq, nq, s->rows)) return SN_ERR_BAD_ARG;
@@ -74,7 +77,7 @@ sn_status check_scan_sizes(const sn_scan_shape *s)
 {
     if (!s || s->channels < 1 || s->states < 1 || s->groups < 1 || s->channels % s->groups || !valid_dtype(s->dtype) || !flag(s->softplus) || !flag(s->ragged))
         return SN_ERR_BAD_ARG;
-    if (s->states > SN_SCAN_MAX_STATES || (int64_t)s->channels * s->states > INT32_MOST) return SN_ERR_UNSUPPORTED;
+    if (s->states > SN_SCAN_MAX_STATES || s->groups * (int64_t)((s->channels / s->groups + 15) / 16) > GRID_Y_MOST) return SN_ERR_UNSUPPORTED;
     return check_rows(s->rows, s->seqs, s->ragged);
 }
 
@@ -117,7 +120,7 @@ sn_status sn_causal_conv1d_fwd(const void *x, const void *w, const float *bias, 
 
 size_t sn_causal_conv1d_scratch_bytes(int64_t rows, int32_t channels, int32_t width)
 {
-    if (rows < 0 || rows > INT32_MOST || channels < 1 || width < 1 || width > SN_CONV1D_MAX_WIDTH || (int64_t)channels * width > INT32_MOST) return 0;
+    if (rows < 0 || rows > ROWS_MOST || channels < 1 || width < 1 || width > SN_CONV1D_MAX_WIDTH || channels > GRID_Y_MOST * 256) return 0;
     return conv1d_scratch_bytes(rows, channels, width);
 }
 
@@ -159,7 +162,7 @@ sn_status sn_headnorm_rot_fwd(const void *q, const void *k, const float *wq, con
 
 size_t sn_headnorm_rot_scratch_bytes(int64_t rows, int32_t q_heads, int32_t k_heads, int32_t head_dim)
 {
-    if (rows < 0 || rows > INT32_MOST || q_heads < 1 || k_heads < 0 || (int64_t)q_heads + k_heads > (1 << 20) || head_dim < 2 || head_dim > SN_HEADNORM_MAX_DIM) return 0;
+    if (rows < 0 || rows > ROWS_MOST || q_heads < 1 || k_heads < 0 || (int64_t)q_heads + k_heads > (1 << 20) || head_dim < 2 || head_dim > SN_HEADNORM_MAX_DIM) return 0;
     return headnorm_scratch_bytes(rows, q_heads, k_heads, head_dim);
 }
 
@@ -201,7 +204,7 @@ sn_status sn_scan_fwd(const void *u, const void *dt, const float *A, const void 
 {
     const sn_status s = check_scan(shape, u, dt, A, B, C, D, z, dt_bias, y);
     if (s != SN_OK) return s;
-    if ((seq_offsets != nullptr) != (shape->ragged != 0) || !aligned(seq_offsets, 4) || !optional(h0, 4) || !optional(hT, 4) || !optional(states, 4) || same(u, y) ||
+    if ((seq_offsets != nullptr) != (shape->ragged != 0) || !aligned(seq_offsets, 4) || !optional(h0, 4) || !optional(hT, 4) || !optional(states, 256) || same(u, y) ||
         same(dt, y) || same(z, y) || overlap(h0, hT, (size_t)shape->seqs * shape->channels * shape->states) || (workspace_bytes && !workspace) ||
         !aligned(workspace, 256))
         return SN_ERR_BAD_ARG;
@@ -217,7 +220,7 @@ sn_status sn_scan_bwd(const void *u, const void *dt, const float *A, const void 
     if (s != SN_OK) return s;
     const size_t e = esize(shape->dtype);
     const int64_t rows = shape->rows, gn = (int64_t)shape->groups * shape->states;
-    if ((seq_offsets != nullptr) != (shape->ragged != 0) || !aligned(seq_offsets, 4) || !optional(h0, 4) || !optional(states, 4) || !optional(dhT, 4) || !optional(dh0, 4) ||
+    if ((seq_offsets != nullptr) != (shape->ragged != 0) || !aligned(seq_offsets, 4) || !optional(h0, 4) || !optional(states, 256) || !optional(dhT, 4) || !optional(dh0, 4) ||
         overlap(dhT, dh0, (size_t)shape->seqs * shape->channels * shape->states) || overlap(h0, dh0, (size_t)shape->seqs * shape->channels * shape->states))
         return SN_ERR_BAD_ARG;
     if (!tensor(du, e, rows) || !tensor(ddt, e, rows) || !tensor(dB, e, rows) || !tensor(dC, e, rows) || !dA || !aligned(dA, 4) || (dD != nullptr) != (D != nullptr) ||

@@ -59,12 +59,12 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
                                                              int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, const T *__restrict__ state_in, T *__restrict__ state_out)
 {
     constexpr int R = 8;   // rows at a time: their loads are all on their way before the first is used
-    const int c = (blockIdx.x * THREADS + threadIdx.x) * V;
-    if (c >= channels) return;
-    Taps<T, V, W> taps;
-    taps.load(w, bias, c);
+    const bool mine = (blockIdx.x * THREADS + threadIdx.x) * V < channels;
+    const int c = mine ? (blockIdx.x * THREADS + threadIdx.x) * V : 0;
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
-    if (r0 < r1) {
+    if (mine && r0 < r1) {
+        Taps<T, V, W> taps;
+        taps.load(w, bias, c);
         SeqAt at = seq_find(rows, r0);
         Pack<T, V> in[W - 1 + R], ahead[R];   // the rows in front, if the last turn was a whole one, and this turn's; the next turn's
         const auto fetch = [&](int b) {
@@ -119,14 +119,14 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
     }
     // the states of empty sequences pass through
     if (state_out && W > 1 && blockIdx.y == 0 && (rows.off || rows.rows == 0))
-        for (int s = 0; s < rows.seqs; ++s) {
-            if (rows.off && rows.off[s] != rows.off[s + 1]) continue;
+        each_empty(rows, [&](int s) {
+            if (!mine) return;
             for (int j = 0; j < W - 1; ++j)
                 for (int i = 0; i < V; ++i) {
                     const int64_t k = ((int64_t)s * (W - 1) + j) * channels + c + i;
                     state_out[k] = state_in ? state_in[k] : (T)0;
                 }
-        }
+        });
 }
 
 // d y / d p

@@ -29,7 +29,7 @@ struct ScanArgs {
     float *hT, *dh0, *states;
     SeqRows rows;
     int channels, N, per_group, blocks_per_group, softplus;
-    int span_rows, chunk_rows, parts, spans, tiles_per_span;  // a span (a sequence, or all rows) in `parts` chunks
+    int span_rows, chunk_rows, parts, spans, tiles_per_span;  // a span (a long sequence, or all rows) in `parts` chunks
     float *carry, *sum_delta;                                 // [chunk][channels][NP], [chunk][channels]
     int *through;                                             // [chunk]: no sequence ends and begins in it
     int NP;                                                   // the states of the library's own arrays: padded to four for each lane
@@ -69,8 +69,8 @@ template <int ROWS> __device__ inline Piece piece_before(const SeqRows &r, SeqAt
     if (at.s >= r.seqs && to > r0) at = seq_clamped(r, r.seqs - 1);
     to = min(to, at.end);
     while (at.s >= 0 && to > r0 && to <= at.begin) {
-        if (!r.off) return p;   // equal lengths: a chunk lies in one sequence
-        at = at.s ? seq_clamped(r, at.s - 1) : SeqAt{-1, 0, 0};
+        if (at.s == 0) at = SeqAt{-1, 0, 0};
+        else at = r.off ? seq_clamped(r, at.s - 1) : SeqAt{at.s - 1, at.begin - r.len, at.begin};
         to = min(to, at.end);
     }
     if (at.s < 0 || to <= r0) return p;
@@ -126,6 +126,13 @@ template <int TOP, int LOW, int COUNT> __device__ inline float scatter_sum(float
     }
 }
 
+// A * log2(e), held within the range: 0 * A has to stay 0 in rows that are not the piece's, also for A = -inf, where all others decay to 0.
+__device__ inline float scan_rate(float A)
+{
+    const float A2 = A * 1.44269504088896340736f;
+    return A2 == -INFINITY ? -3.402823466e38f : A2;
+}
+
 // The lane's channel of a group's block, its states, and what is fixed of them.
 template <int NL> struct ScanLane {
     int c, n0, channel;   // channel within the workgroup's, first state, channel of the tensors
@@ -139,7 +146,7 @@ template <int NL> struct ScanLane {
         there = c < nch;
         channel = c0 + c;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) A2[i] = there && n0 + i < a.N ? a.A[(int64_t)channel * a.N + n0 + i] * 1.44269504088896340736f : 0.f;
+        for (int i = 0; i < 4; ++i) A2[i] = there && n0 + i < a.N ? scan_rate(a.A[(int64_t)channel * a.N + n0 + i]) : 0.f;
     }
     // Four states of one of the library's own arrays, [..][channels][NP]: padded, so that they are one access.  In two steps: a load without a
     // condition, and the choice of what is there.

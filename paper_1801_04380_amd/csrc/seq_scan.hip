@@ -51,8 +51,8 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
     if (!LOCAL && part > 0) lane.load_own(a.carry, chunk, a, h);
 
     if (r0 < r1) {
-        SeqAt at = seq_find(a.rows, r0);
-        Piece next = piece_from<ROWS>(a.rows, at, r0, r0, r1);
+        SeqAt at = seq_find(a.rows, LOCAL ? r1 - 1 : r0);   // a chunk hands on the state of the sequence that holds its last row
+        Piece next = piece_from<ROWS>(a.rows, at, LOCAL ? max(r0, at.begin) : r0, r0, r1);
         Staged<T, NL, WHOLE> u[RP], dt[RP], z[RP];
         StagedBC<T, NL, ROWS, OUT, WHOLE> BC;
         const auto fetch = [&]() {
@@ -170,12 +170,11 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
         if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
     }
     if (OUT && a.hT && chunk == 0 && (a.rows.off || a.rows.rows == 0))
-        for (int s = 0; s < a.rows.seqs; ++s) {   // the states of empty sequences pass through
-            if (a.rows.off && a.rows.off[s] != a.rows.off[s + 1]) continue;
+        each_empty(a.rows, [&](int s) {   // their states pass through
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             if (a.h0) lane.load(a.h0, s, a, v);
             lane.store(a.hT, s, a, v);
-        }
+        });
 }
 
 // The state that each chunk starts from, in place of the one that it ends with from zero.  Reverse: the gradient of the state that
@@ -185,20 +184,28 @@ __global__ void __launch_bounds__(THREADS) scan_carry_kernel(ScanArgs a, int rev
     const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.NP;
     if (i >= each) return;
     const int channel = (int)(i / a.NP), n = (int)(i % a.NP);
-    const float A2 = n < a.N ? a.A[(int64_t)channel * a.N + n] * 1.44269504088896340736f : 0.f;
+    const float A2 = n < a.N ? scan_rate(a.A[(int64_t)channel * a.N + n]) : 0.f;
     float v = 0.f;
-    for (int k = 0; k < a.parts; ++k) {
-        const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - k : k);
-        float local = 0.f;
-        bool through = false;
-        float sum = 0.f;
-        if (k < a.parts - 1) {
-            local = a.carry[chunk * each + i];
-            through = a.through[chunk];
-            sum = a.sum_delta[chunk * a.channels + channel];
+    constexpr int AT = 8;   // chunks whose values are on their way together (the pass over 32768 x 1024 x 16: 256 us, one by one 271)
+    for (int k0 = 0; k0 < a.parts; k0 += AT) {
+        float local[AT], sum[AT];
+        int through[AT];
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            const int at = min(k0 + k, a.parts - 2);   // the last one hands on to nothing: it has no values
+            const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - at : at);
+            local[k] = a.carry[chunk * each + i];
+            through[k] = a.through[chunk];
+            sum[k] = a.sum_delta[chunk * a.channels + channel];
         }
-        a.carry[chunk * each + i] = v;
-        v = through ? fmaf(exp2_fast(A2 * sum), v, local) : local;
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            if (k0 + k >= a.parts) break;
+            const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - k0 - k : k0 + k);
+            a.carry[chunk * each + i] = v;
+            // a state of 0 stays 0, also through a factor past the range (growing states before the first input)
+            v = through[k] && v != 0.f ? fmaf(exp2_fast(A2 * sum[k]), v, local[k]) : local[k];
+        }
     }
 }
 
@@ -286,7 +293,10 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
     p.CB = 256 / p.NL;
     p.blocks_per_group = div_up(s.channels / s.groups, p.CB);
     p.blocks = p.blocks_per_group * s.groups;
-    p.spans = s.ragged || s.rows == 0 ? 1 : s.seqs;
+    // Sequences of equal length are walked each on its own, unless they are no longer than a tile: kept states and sums would be one for
+    // each, where a tile holds several.  4096 x 4 rows of 2048 x 16, us forward and backward, MB of states and workspace: on their own 879, 4054,
+    // 1152, together 718, 1724, 200; 1024 x 16 rows 278, 1140, 336 and 269, 678, 200.
+    p.spans = s.ragged || s.rows / s.seqs <= TS ? 1 : s.seqs;
     p.span_rows = (int)(s.rows / p.spans);
     p.tiles_per_span = div_up(p.span_rows, TS);
     if (parts < 1) parts = 1;
@@ -297,14 +307,18 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
     return p;
 }
 
-// Into how many chunks a span is cut when there is workspace for it.
+// Into how many chunks a span is cut when there is workspace for it: a SIMD holds four waves of the forward kernels (a workgroup has
+// one for each) and two of the backward one, and a wave alone leaves more than half of its issue slots empty; twice as many, so that they
+// do not all end together; two tiles each at least.  us with 256, 512, 1024, 2048, 4096 workgroups: forward over 32768 x 1024
+// x 16 501, 320, 264, 256, 267, over 17 ragged sequences, 6000 x 2048 x 16, 209, 144, 127, 123, 137; forward and backward with 256, 512,
+// 1024, 2048 in the backward pass, 8 x 2048 x 2048 x 16 1029, 943, 913, 909, 8193 x 512 x 32 335, 275, 286, 299.
 int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
 {
     const ScanPlan p = scan_plan(s, 1);
-    const int64_t have = (int64_t)p.blocks * p.spans, want = bwd ? 512 : 1024;
+    const int64_t have = (int64_t)p.blocks * p.spans, want = bwd ? 1024 : 2048;
     if (have >= want) return 1;
     int64_t parts = (want + have - 1) / have;
-    const int64_t most = p.tiles_per_span / 4;   // chunks of 64 rows at least
+    const int64_t most = p.tiles_per_span / 2;
     if (parts > most) parts = most;
     return parts < 1 ? 1 : (int)parts;
 }

@@ -46,8 +46,8 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     for (int i = 0; i < VE; ++i) bias[i] = a.bias && i < nco ? a.bias[c0 + co + i] : 0.f;
     float g[4] = {0.f, 0.f, 0.f, 0.f}, sum_delta = 0.f;
     bool crossed = false;
-    SeqAt at = seq_find(a.rows, r1 - 1);
-    Piece next = piece_before<TS>(a.rows, at, r1, r0);
+    SeqAt at = seq_find(a.rows, r0);   // a chunk hands on the gradient of the sequence that holds its first row
+    Piece next = piece_before<TS>(a.rows, at, min(r1, at.end), r0);
     Staged<T, NL, WHOLE> dt, z, dy;
     StagedBC<T, NL, TS, false, WHOLE> C;
     const char *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T), *pdy = (const char *)a.dy + c0 * sizeof(T);
@@ -363,19 +363,18 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
         if (c < nch) (k < CB ? a.part_d : a.part_bias)[(int64_t)chunk * a.channels + c0 + c] = sum;
     }
     if (a.dh0 && chunk == 0 && (a.rows.off || a.rows.rows == 0))
-        for (int s = 0; s < a.rows.seqs; ++s) {   // through empty sequences
-            if (a.rows.off && a.rows.off[s] != a.rows.off[s + 1]) continue;
+        each_empty(a.rows, [&](int s) {   // the gradients of their states pass through
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             if (a.dhT) lane.load(a.dhT, s, a, v);
             lane.store(a.dh0, s, a, v);
-        }
+        });
 }
 
 // dB and dC from the sums of the channel blocks: one thread per row, group, tensor and state.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int groups, int NP)
 {
-    const int64_t k = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+    const int64_t k = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * THREADS + threadIdx.x;
     const int n = (int)(k % NP), which = (int)(k / NP % 2), group = (int)(k / (2 * NP) % groups);
     const int64_t row = k / (2 * NP) / groups;
     if (row >= a.rows.rows || n >= a.N) return;
@@ -475,7 +474,8 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     if (e != hipSuccess) return e;
     if (s.rows) {
         const int64_t n = s.rows * s.groups * 8 * p.NL;
-        const unsigned blocks = (unsigned)((n + THREADS - 1) / THREADS);
+        const int64_t all = (n + THREADS - 1) / THREADS, most = 1 << 20;   // in x: a dimension of a grid has to stay below 2^32 threads
+        const dim3 blocks((unsigned)(all < most ? all : most), (unsigned)((all + most - 1) / most));
         if (bf16) scan_join_kernel<bf16_t><<<blocks, THREADS, 0, st>>>(a, s.groups, 4 * p.NL);
         else scan_join_kernel<float><<<blocks, THREADS, 0, st>>>(a, s.groups, 4 * p.NL);
         e = hipGetLastError();

@@ -352,6 +352,257 @@ def test_nan_of_one_sequence_stays_in_it():
     close(g["dh0"][[0, 2]], want["dh0"][[0, 2]])
 
 
+@pytest.mark.parametrize("dtype,S,L,N", [("bf16", 300, 4, 16), ("f32", 41, 16, 8), ("f32", 90, 1, 32), ("bf16", 23, 15, 5)])
+def test_scan_of_many_short_sequences_of_equal_length(dtype, S, L, N):
+    """They share tiles and chunks; as ragged sequences and as equal ones the rows are cut in the same way, so the results are the same."""
+    c = Scan(dtype, [L] * S, S * L, 24, N, 1, S)
+    y, hT, want = c.want()
+    kept = []
+    for off in (None, offsets([L] * S)):
+        kw, shape = {"seqs": S, "offsets": off}, c.shape(off is not None)
+        fwd, bwd = sn.sn_scan_workspace_query(shape, sn.SN_SCAN_FWD)[1], sn.sn_scan_workspace_query(shape, sn.SN_SCAN_BWD)[1]
+        states = bytes_(sn.sn_scan_states_bytes(shape))
+        gy, gh = c.forward(kw, states, bytes_(fwd))
+        gy.check(y)
+        close(gh, hT)
+        g = c.backward(kw, bytes_(bwd), states)
+        c.check(g, want)
+        kept.append([gy.wide, gh] + [v.wide if isinstance(v, Out) else v for v in g.values() if v is not None])
+    assert all(torch.equal(a, b) for a, b in zip(*kept))
+
+
+def test_scan_of_many_sequences_most_of_them_empty():
+    """More than the 64 offsets that a wave looks at together, rows of three sequences and behind the last."""
+    lengths = [0] * 70 + [19] + [0] * 131 + [1] + [0] * 64 + [45] + [0] * 3
+    c = Scan("f32", lengths, 70, 20, 16, 1, 8)
+    kw, shape = {"seqs": len(lengths), "offsets": offsets(lengths)}, c.shape(True)
+    y, hT, want = c.want()
+    gy, gh = c.forward(kw, None, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_FWD)[1]))
+    gy.check(y)
+    close(gh, hT)
+    c.check(c.backward(kw, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_BWD)[1] + sn.sn_scan_states_bytes(shape))), want)
+
+
+def test_scan_states_that_grow_or_vanish_at_once():
+    """A > 0: a chunk's factor leaves the range while the state is still zero, as nothing has come in.  A = -inf: nothing is kept from one
+    token to the next, also where a sequence ends inside a tile.  The answers are whole numbers."""
+    rows, D, N = 700, 8, 4
+    u = torch.zeros(rows, D, device="cuda")
+    u[-1] = 2.0
+    dt = torch.full((rows, D), 4.0, device="cuda")                     # e^4 a token, 2^184 a chunk of 32
+    B, C = torch.ones(rows, N, device="cuda"), torch.ones(rows, N, device="cuda")
+    A = torch.tensor([1.0, float("-inf"), 0.0, -1.0], device="cuda").repeat(D, 1)
+    y, hT = torch.empty(rows, D, device="cuda"), torch.empty(1, D, N, device="cuda")
+    ws = bytes_(sn.sn_scan_workspace_query(sn.scan_shape(rows, D, N, 1, 1, sn.SN_F32, False, False), sn.SN_SCAN_FWD)[1])
+    sn.sn_scan_fwd(u, dt, A, B, C, None, None, None, y, hT=hT, workspace=ws, softplus=False)
+    assert ws is not None and (y[:-1] == 0).all() and (y[-1] == 32).all() and (hT == 8).all()   # delta u B = 8 in each of four states
+    u[:] = 1.0
+    A[:] = float("-inf")
+    off = offsets([0, 350, 340])
+    y.fill_(SENTINEL)
+    sn.sn_scan_fwd(u, dt, A, B, C, None, None, None, y, offsets=off, seqs=3, workspace=ws, softplus=False)
+    assert (y[:690] == 16).all() and (y[690:] == SENTINEL).all()
+
+
+# ---- streams, graphs, large tensors ----
+class Chain:
+    """The calls of the three operators, forward and backward, one feeding the next, on buffers made once: for streams and graphs."""
+
+    def __init__(self, seed, dtype=torch.bfloat16):
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.lengths, self.E, self.N = [300, 0, 77, 1, 130], 64, 16
+        self.rows, S = 520, 5                                           # 12 rows behind the last sequence
+        r = lambda *n, t=dtype: torch.randn(*n, generator=self.g, device="cuda").to(t)  # noqa: E731
+        z = lambda *n, t=dtype: torch.zeros(*n, device="cuda", dtype=t)  # noqa: E731
+        f, R, E, N = torch.float32, self.rows, self.E, self.N
+        self.x, self.z, self.q, self.k, self.dt, self.dy = r(R, E), r(R, E), r(R, N), r(R, N), r(R, E), r(R, E)
+        self.w, self.bias, self.wn = r(E, 4), r(E, t=f), r(N, t=f)
+        self.A, self.D, self.db = -torch.rand(E, N, generator=self.g, device="cuda"), r(E, t=f), r(E, t=f) - 3
+        self.freq, self.off = torch.rand(N // 2, generator=self.g, device="cuda"), offsets(self.lengths)
+        self.h0, self.dhT, self.s0 = r(S, E, N, t=f), r(S, E, N, t=f), r(S, 3, E)
+        self.u, self.B, self.C, self.y, self.hT, self.s1 = z(R, E), z(R, N), z(R, N), z(R, E), z(S, E, N, t=f), z(S, 3, E)
+        self.du, self.ddt, self.dB, self.dC, self.dz, self.dq, self.dk, self.dx = z(R, E), z(R, E), z(R, N), z(R, N), z(R, E), z(R, N), z(R, N), z(R, E)
+        self.grads = [z(E, N, t=f), z(E, t=f), z(E, t=f), z(S, E, N, t=f), z(N, t=f), z(N, t=f), z(E, 4, t=f), z(E, t=f), z(S, 3, E)]
+        shape = sn.scan_shape(R, E, N, 1, S, sn.SN_BF16, True)
+        self.states = bytes_(sn.sn_scan_states_bytes(shape))
+        self.ws = [bytes_(sn.sn_scan_workspace_query(shape, i)[1]) for i in (sn.SN_SCAN_FWD, sn.SN_SCAN_BWD)]
+        self.hs, self.cs = bytes_(sn.sn_headnorm_rot_scratch_bytes(R, 1, 1, N)), bytes_(sn.sn_causal_conv1d_scratch_bytes(R, E, 4))
+
+    def run(self):
+        kw, (dA, dD, ddb, dh0, dwq, dwk, dw, dbias, ds0) = {"seqs": 5, "offsets": self.off}, self.grads
+        sn.sn_causal_conv1d_fwd(self.x, self.w, self.bias, self.u, state_in=self.s0, state_out=self.s1, **kw)
+        sn.sn_headnorm_rot_fwd(self.q, self.k, self.wn, self.wn, None, self.freq, self.C, self.B, self.N)
+        args = (self.u, self.dt, self.A, self.B, self.C, self.D, self.z, self.db)
+        sn.sn_scan_fwd(*args, self.y, h0=self.h0, hT=self.hT, states=self.states, workspace=self.ws[0], **kw)
+        sn.sn_scan_bwd(*args, self.dy, self.du, self.ddt, dA, self.dB, self.dC, dD, self.dz, ddb, self.ws[1], h0=self.h0, states=self.states, dhT=self.dhT, dh0=dh0, **kw)
+        sn.sn_headnorm_rot_bwd(self.q, self.k, self.wn, self.wn, None, self.freq, self.dC, self.dB, self.dq, self.dk, dwq, dwk, self.hs, self.N)
+        sn.sn_causal_conv1d_bwd(self.x, self.w, self.bias, self.du, self.dx, dw, dbias, self.cs, state_in=self.s0, dstate_in=ds0, **kw)
+
+    def outputs(self):
+        return [self.u, self.B, self.C, self.y, self.hT, self.s1, self.du, self.ddt, self.dB, self.dC, self.dz, self.dq, self.dk, self.dx] + self.grads
+
+    def take(self):
+        return [t.clone() for t in self.outputs()]
+
+    def poison(self):
+        """Outputs and workspaces hold something else before the next run."""
+        for t in self.outputs():
+            t.fill_(SENTINEL)
+        for t in [self.states, self.hs, self.cs] + self.ws:
+            t.fill_(255)
+
+
+def test_results_are_the_same_from_run_to_run():
+    c = Chain(1)
+    c.poison()
+    c.run()
+    first = c.take()
+    for _ in range(4):
+        c.poison()
+        c.run()
+        assert all(torch.equal(a, b) for a, b in zip(c.outputs(), first))
+
+
+def test_calls_run_on_the_current_stream():
+    c = Chain(2)
+    c.poison()
+    c.run()
+    want = c.take()
+    x = c.x.clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        c.poison()
+        c.x.zero_()
+        torch.cuda._sleep(2_000_000)     # the input arrives on this stream, behind this
+        c.x.copy_(x)
+        c.run()
+        got = c.take()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_captured_calls_replay():
+    """Two graphs, each with its own buffers and workspaces, replayed by turns and side by side with new inputs, against eager runs."""
+    chains, graphs = [Chain(3), Chain(4)], []
+    for c in chains:
+        c.run()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.run()
+        graphs.append(graph)
+    for turn in range(4):
+        want = []
+        for c in chains:
+            for t in (c.x, c.z, c.q, c.dt, c.dy):
+                t.copy_(torch.randn(t.shape, generator=c.g, device="cuda"))
+            c.poison()
+            c.run()
+            want.append(c.take())
+            c.poison()
+        torch.cuda.synchronize()
+        if turn % 2:
+            streams = [torch.cuda.Stream() for _ in chains]
+            for graph, stream in zip(graphs, streams):
+                with torch.cuda.stream(stream):
+                    graph.replay()
+        else:
+            for graph in graphs:
+                graph.replay()
+        torch.cuda.synchronize()
+        for c, w in zip(chains, want):
+            assert all(torch.equal(a, b) for a, b in zip(c.outputs(), w)), turn
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    """Columns of one tensor of 2^31 elements and more: the last rows lie beyond what 32 bits count, in elements as in bytes.  The calls'
+    results are those of the same rows side by side."""
+    ld, rows, E, N = (1 << 20) + 64, 2200, 64, 16
+    assert ld * rows > 1 << 31
+    wide = torch.empty(rows, ld, dtype=torch.bfloat16, device="cuda")
+    at = iter(range(0, ld, ld // 32 // 64 * 64))
+    c = Chain(5)
+    c.rows, near = rows, {}
+    gen = lambda n: torch.randn(rows, n, generator=c.g, device="cuda").bfloat16()  # noqa: E731
+    names = dict(x=E, z=E, q=N, k=N, dt=E, dy=E, u=E, B=N, C=N, y=E, du=E, ddt=E, dB=N, dC=N, dz=E, dq=N, dk=N, dx=E)
+    shape = sn.scan_shape(rows, E, N, 1, 5, sn.SN_BF16, True)
+    c.states = bytes_(sn.sn_scan_states_bytes(shape))
+    c.ws = [bytes_(sn.sn_scan_workspace_query(shape, i)[1]) for i in (sn.SN_SCAN_FWD, sn.SN_SCAN_BWD)]
+    c.hs, c.cs = bytes_(sn.sn_headnorm_rot_scratch_bytes(rows, 1, 1, N)), bytes_(sn.sn_causal_conv1d_scratch_bytes(rows, E, 4))
+    c.off = offsets([900, 0, 77, 1, rows - 978])
+    for n, width in names.items():
+        near[n] = gen(width)
+        setattr(c, n, near[n])
+    c.run()
+    want = c.take()
+    for n, width in names.items():
+        lead = next(at)
+        t = wide[:, lead:lead + width]
+        t.copy_(near[n])
+        setattr(c, n, t)
+    c.poison()
+    c.run()
+    assert all(torch.equal(a, b) for a, b in zip(c.outputs(), want))
+
+
+def test_pools_of_states_whose_offsets_pass_32_bits():
+    D, N, W = 4096, 16, 4
+    slots = (1 << 31) // (D * N) + 2
+    d = Data("f32", 9)
+    pick = torch.tensor([slots - 1, 0, slots, slots - 2], dtype=torch.int32)       # the third is a row to skip
+    x, B, C, h = d.normal(4, D), d.normal(4, N), d.normal(4, N), d.normal(2, D, N)
+    A = -torch.rand(D, N, generator=d.g)
+    pool = torch.empty(slots, D, N, device="cuda")
+    pool[slots - 2:] = h.cuda()
+    pool[0] = h[0].cuda()
+    y = torch.full((4, D), SENTINEL, device="cuda")
+    sn.sn_scan_step(x.cuda(), x.cuda(), A.cuda(), B.cuda(), C.cuda(), None, None, None, y, pool, slots=pick.cuda())
+    for row, start in ((0, h[1]), (1, h[0]), (3, h[0])):
+        f = lambda t: f64(t)[row:row + 1]  # noqa: E731
+        wy, wh = oracle.scan_fwd(f(x), f(x), f64(A), f(B), f(C), None, None, None, [1], f64(start)[None])
+        close(y[row:row + 1], wy)
+        close(pool[int(pick[row])][None], wh)
+    assert (y[2] == SENTINEL).all()
+    del pool
+    slots = (1 << 31) // (D * (W - 1)) + 2
+    pool = torch.empty(slots, W - 1, D, dtype=torch.bfloat16, device="cuda")
+    state, x, w = d.normal(2, W - 1, D, dtype=torch.bfloat16), d.normal(2, D, dtype=torch.bfloat16), d.normal(D, W, dtype=torch.bfloat16)
+    pool[slots - 2:] = state.cuda()
+    y = torch.empty(2, D, dtype=torch.bfloat16, device="cuda")
+    sn.sn_causal_conv1d_step(x.cuda(), w.cuda(), None, y, pool, slots=torch.tensor([slots - 2, slots - 1], dtype=torch.int32, device="cuda"))
+    wy, ws = oracle.conv1d_fwd(f64(x), f64(w), None, [1, 1], f64(state))
+    close(y, wy, torch.bfloat16)
+    assert np.array_equal(f64(pool[slots - 2:]), ws)
+
+
+def test_kept_states_whose_offsets_pass_32_bits():
+    """The states before every 16th token are more than 2^31 elements: a last short sequence behind a long one has the results that it has alone."""
+    D, N, S = 2048, 64, 2
+    rows, last = (1 << 31) // (D * N) * 16 + 32 + 50, 50
+    g = torch.Generator(device="cuda").manual_seed(12)
+    r = lambda n, m: torch.randn(n, m, generator=g, device="cuda")  # noqa: E731
+    ins = {"u": r(rows, D), "dt": r(rows, D), "B": r(rows, N), "C": r(rows, N), "dy": r(rows, D)}
+    A = -torch.arange(1, N + 1, device="cuda").float().repeat(D, 1)
+
+    def both(t, seqs, off):
+        shape = sn.scan_shape(t["u"].shape[0], D, N, 1, seqs, sn.SN_F32, True)
+        new = lambda k: torch.empty_like(t[k])  # noqa: E731
+        states = torch.empty(sn.sn_scan_states_bytes(shape), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(max(sn.sn_scan_workspace_query(shape, i)[1] for i in (0, 1)), dtype=torch.uint8, device="cuda")
+        y, du, ddt, dB, dC, dA = new("u"), new("u"), new("dt"), new("B"), new("C"), torch.empty_like(A)
+        args = (t["u"], t["dt"], A, t["B"], t["C"], None, None, None)
+        sn.sn_scan_fwd(*args, y, offsets=off, seqs=seqs, states=states, workspace=ws)
+        sn.sn_scan_bwd(*args, t["dy"], du, ddt, dA, dB, dC, None, None, None, ws, offsets=off, seqs=seqs, states=states)
+        return states.numel(), [y, du, ddt, dB, dC]
+
+    n, far = both(ins, S, offsets([rows - last, last]))
+    assert n > 4 << 31
+    _, near = both({k: v[rows - last:].contiguous() for k, v in ins.items()}, 1, offsets([last]))
+    for a, b in zip(far, near):
+        close(a[rows - last:], f64(b))
+
+
 # ---- together ----
 def test_mixer_forward_and_backward():
     """Convolution of a projection's slice, norm and rotation of B and C, scan with gate; then all the gradients, each call fed by the one

@@ -185,3 +185,39 @@ def test_binding_refuses_what_does_not_fit():
         sn.sn_headnorm_rot_fwd(x, None, None, None, None, None, torch.zeros(4, 8), None, 3)
     with pytest.raises(ValueError, match="whole groups"):
         sn.sn_scan_fwd(x, x, torch.zeros(8, 3), x, x, None, None, None, torch.zeros(4, 8))
+
+
+def test_kept_states_are_aligned():
+    P8 = ctypes.c_void_p(P[12].value + 8)
+    assert scan(_sfwd, 14, p12=P8) == BAD and scan(_sbwd, 23, p19=ctypes.c_void_p(P[19].value + 16)) == BAD
+
+
+@pytest.mark.parametrize("field", ["u", "dt", "b", "c", "z", "y"])
+def test_scan_refuses_rows_too_far_apart(field):
+    kw = {"ld_" + field: (1 << 24) + 1}
+    assert scan(_sfwd, 14, **kw) == UNSUPPORTED and scan(_sbwd, 23, **kw) == UNSUPPORTED and scan(_sstep, 12, **kw) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("field", ["du", "ddt", "db", "dc", "dz"])
+def test_scan_refuses_gradients_rows_too_far_apart(field):
+    assert scan(_sbwd, 23, **{"ld_" + field: (1 << 24) + 1}) == UNSUPPORTED
+
+
+def test_sizes_beyond_the_grids():
+    most, rows = 65535, 1 << 30
+    big = lambda n: {"ld_" + f: n for f in ("u", "dt", "b", "c", "z", "y", "du", "ddt", "db", "dc", "dz")}  # noqa: E731
+    assert scan(_sfwd, 14, rows=rows + 1) == UNSUPPORTED and scan(_sbwd, 23, rows=rows + 1) == UNSUPPORTED
+    assert scan(_sfwd, 14, seqs=1 << 24) == UNSUPPORTED and scan(_sbwd, 23, seqs=1 << 24) == UNSUPPORTED
+    assert scan(_sfwd, 14, channels=most * 16 + 1, groups=1, **big(1 << 24)) == UNSUPPORTED
+    assert scan(_sfwd, 14, channels=40000 * 17, groups=40000, states=1, **big(1 << 24)) == UNSUPPORTED      # two blocks a group
+    assert scan(_sstep, 12, rows=1 << 24) == UNSUPPORTED
+    assert conv(_fwd, 7, channels=most * 256 + 1, ld_x=1 << 25, ld_y=1 << 25, ld_dx=1 << 25) == UNSUPPORTED
+    assert conv(_step, 7, rows=1 << 24) == UNSUPPORTED and conv(_fwd, 7, seqs=1 << 24) == UNSUPPORTED
+    assert heads(_hfwd, rows=rows + 1) == UNSUPPORTED
+    assert sn.sn_causal_conv1d_scratch_bytes(rows + 1, 4, 4) == 0 == sn.sn_headnorm_rot_scratch_bytes(rows + 1, 1, 0, 16)
+
+
+def test_short_sequences_of_equal_length_share_tiles():
+    together = sn.scan_shape(64 * 4, 64, 16, seqs=64)
+    assert sn.sn_scan_states_bytes(together) == 64 * 4 // 16 * 64 * 16 * 4
+    assert sn.sn_scan_states_bytes(sn.scan_shape(64 * 17, 64, 16, seqs=64)) == 64 * 2 * 64 * 16 * 4
