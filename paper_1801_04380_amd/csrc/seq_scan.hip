@@ -178,35 +178,47 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
 }
 
 // The state that each chunk starts from, in place of the one that it ends with from zero.  Reverse: the gradient of the state that
-// reaches a chunk from the one behind it.
-__global__ void __launch_bounds__(THREADS) scan_carry_kernel(ScanArgs a, int reverse)
+// reaches a chunk from the one behind it.  A thread takes one value along the chunks; bound by the latency of its loads, 16 chunks' at a time.
+// 1024 x 16 values through 128 chunks take 16 us (8 at a time 18; 32 need more scalar registers than there are, 56); 16 threads for
+// each value, joined through LDS, take 12 there, but 51 instead of 6 where 8 sequences of 2048 x 16 values have 8 chunks each.
+__global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a, int reverse)
 {
-    const int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x, each = (int64_t)a.channels * a.NP;
+    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, each = (int64_t)a.channels * a.NP;
     if (i >= each) return;
     const int channel = (int)(i / a.NP), n = (int)(i % a.NP);
     const float A2 = n < a.N ? scan_rate(a.A[(int64_t)channel * a.N + n]) : 0.f;
+    const int64_t first = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 : 0), dir = reverse ? -1 : 1, step = dir * each, row = dir * a.channels;
+    const float *from = a.carry + first * each + i, *sums = a.sum_delta + first * a.channels + channel;
+    const int *pass = a.through + first;
+    float *to = a.carry + first * each + i;
     float v = 0.f;
-    constexpr int AT = 8;   // chunks whose values are on their way together (the pass over 32768 x 1024 x 16: 256 us, one by one 271)
-    for (int k0 = 0; k0 < a.parts; k0 += AT) {
+    const auto chunks = [&](auto COUNT) {   // so many, their values on their way together
+        constexpr int AT = COUNT.value;
         float local[AT], sum[AT];
         int through[AT];
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            const int at = min(k0 + k, a.parts - 2);   // the last one hands on to nothing: it has no values
-            const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - at : at);
-            local[k] = a.carry[chunk * each + i];
-            through[k] = a.through[chunk];
-            sum[k] = a.sum_delta[chunk * a.channels + channel];
+            local[k] = *from;
+            sum[k] = *sums;
+            through[k] = *pass;
+            from += step;
+            sums += row;
+            pass += dir;
         }
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            if (k0 + k >= a.parts) break;
-            const int64_t chunk = (int64_t)blockIdx.y * a.parts + (reverse ? a.parts - 1 - k0 - k : k0 + k);
-            a.carry[chunk * each + i] = v;
+            *to = v;
+            to += step;
             // a state of 0 stays 0, also through a factor past the range (growing states before the first input)
-            v = through[k] && v != 0.f ? fmaf(exp2_fast(A2 * sum[k]), v, local[k]) : local[k];
+            const float in = keep_if(through[k], v), factor = keep_if(in != 0.f, exp2_fast(A2 * sum[k]));
+            v = fmaf(factor, in, local[k]);
         }
-    }
+    };
+    int k = 0;   // the last chunk hands on to nothing: it has no values
+    for (; k + 16 < a.parts; k += 16) chunks(ScanInt<16>());
+    for (; k + 4 < a.parts; k += 4) chunks(ScanInt<4>());
+    for (; k + 1 < a.parts; ++k) chunks(ScanInt<1>());
+    *to = v;
 }
 
 // One token: a thread holds four states of a channel, NL neighbouring threads a channel.  Bound by reading and writing the states.  WHOLE: a
@@ -377,7 +389,7 @@ void scan_fwd_bytes(const sn_scan_shape &s, size_t *preferred_bytes) { *preferre
 
 hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st)
 {
-    scan_carry_kernel<<<dim3(div_up((int64_t)a.channels * a.NP, THREADS), p.spans), THREADS, 0, st>>>(a, reverse);
+    scan_carry_kernel<<<dim3(div_up((int64_t)a.channels * a.NP, 64), p.spans), 64, 0, st>>>(a, reverse);
     return hipGetLastError();
 }
 

@@ -386,21 +386,28 @@ __global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int grou
     seq_st((T *)to + group * a.N + n, sum);
 }
 
-// dA, dD and the bias's gradient from the sums of the chunks.
+// dA, dD and the bias's gradient from the sums of the chunks: 16 threads along the chunks of each value, joined in a fixed order.
 __global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunks, float *__restrict__ dA, float *__restrict__ dD, float *__restrict__ dbias)
 {
-    int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-    const int64_t each = (int64_t)a.channels * a.N;
-    const float *from;
-    float *to;
-    int64_t at, stride;
+    __shared__ float sums[16][16];
+    const int lane = threadIdx.x / 16;
+    const int64_t i = (int64_t)blockIdx.x * 16 + threadIdx.x % 16, each = (int64_t)a.channels * a.N;
+    const float *from = a.part_a;
+    float *to = nullptr;
+    int64_t at = 0, stride = a.channels;
     if (i < each) { from = a.part_a + i / a.N * (a.NP - a.N); to = dA; at = i; stride = (int64_t)a.channels * a.NP; }
-    else if (i < each + a.channels) { from = a.part_d; to = dD; at = i - each; stride = a.channels; }
-    else if (i < each + 2 * (int64_t)a.channels) { from = a.part_bias; to = dbias; at = i - each - a.channels; stride = a.channels; }
-    else return;
-    if (!to) return;
+    else if (i < each + a.channels) { from = a.part_d; to = dD; at = i - each; }
+    else if (i < each + 2 * (int64_t)a.channels) { from = a.part_bias; to = dbias; at = i - each - a.channels; }
     float sum = 0.f;
-    for (int c = 0; c < chunks; ++c) sum += from[c * stride + at];
+    if (to)
+#pragma unroll 8
+        for (int c = lane; c < chunks; c += 16) sum += from[c * stride + at];
+    sums[lane][threadIdx.x % 16] = sum;
+    __syncthreads();
+    if (lane || !to) return;
+    sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < 16; ++c) sum += sums[c][threadIdx.x];
     to[at] = sum;
 }
 
@@ -482,7 +489,7 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
         if (e != hipSuccess) return e;
     }
     const int64_t n = (int64_t)s.channels * (s.states + 2);
-    scan_sum_kernel<<<(unsigned)((n + THREADS - 1) / THREADS), THREADS, 0, st>>>(a, p.chunks, g.dA, g.dD, g.ddt_bias);
+    scan_sum_kernel<<<(unsigned)((n + 15) / 16), THREADS, 0, st>>>(a, p.chunks, g.dA, g.dD, g.ddt_bias);
     return hipGetLastError();
 }
 
