@@ -11,7 +11,7 @@ template <> __device__ inline float seq_ld<bf16_t>(const bf16_t *p) { return bf1
 __device__ inline void seq_st(float *p, float v) { *p = v; }
 __device__ inline void seq_st(bf16_t *p, float v) { *p = f32_to_bf16(v); }
 
-// V neighbouring elements as they lie in memory, loaded and stored in one access at their size's alignment.  What a lane has nothing to load
+// V neighbouring elements as they lie in memory, loaded and stored in one access, at an element's alignment: global memory takes them there.  What a lane has nothing to load
 // from it loads from some other place and leaves out later: a load under a condition of the lane's own would be waited for right
 // where the two ways meet, and nothing could be loaded ahead.
 template <int BYTES> struct Word;
@@ -21,23 +21,18 @@ template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_typ
 template <> struct Word<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack {
     typedef typename Word<sizeof(T) * V>::type W;   // the access, as one value: a copy of the elements would be split up and stored in parts
+    struct __attribute__((packed, aligned(sizeof(T)))) At { W v; };
     T e[V];
     __device__ void zero()
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) e[i] = 0;
     }
-    __device__ void load(const T *p) { *this = __builtin_bit_cast(Pack, *reinterpret_cast<const W *>(p)); }
-    __device__ void store(T *p) const { *reinterpret_cast<W *>(p) = __builtin_bit_cast(W, *this); }
+    __device__ void load(const T *p) { *this = __builtin_bit_cast(Pack, reinterpret_cast<const At *>(p)->v); }
+    __device__ void store(T *p) const { reinterpret_cast<At *>(p)->v = __builtin_bit_cast(W, *this); }
     __device__ float get(int i) const { return seq_ld<T>(&e[i]); }
     __device__ void set(int i, float v) { seq_st(&e[i], v); }
 };
-
-// Whether rows that are `ld` elements apart can be accessed V elements at a time.
-inline bool rows_aligned(const void *p, int64_t ld, int esize, int v)
-{
-    return reinterpret_cast<uintptr_t>(p) % (size_t)(esize * v) == 0 && ld % v == 0;
-}
 
 // The rows of packed sequences: off == nullptr: `seqs` sequences of `len` rows.  A row of no sequence has s outside 0 .. seqs - 1.  begin
 // and end stay within 0 .. rows whatever the offsets hold.

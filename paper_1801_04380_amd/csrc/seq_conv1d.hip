@@ -1,10 +1,10 @@
 // The short causal convolution along the tokens (one filter of up to 8 taps per channel, bias and SiLU in the same pass).
 //
 // Two multiplications per tap and a sigmoid per element against two or three tensors read and written: bound by HBM.  A thread owns
-// V neighbouring channels (16 bytes where the rows allow it) and walks down a run of rows with the taps' inputs in registers, so that an
+// V neighbouring channels (16 bytes if there are as many; the last thread's are moved back to end with the row, and what it has in common with
+// the thread before it is computed and written twice alike) and walks down a run of rows with the taps' inputs in registers, so that an
 // input row is loaded once but for the width - 1 rows in front of the run.
 #include "seq.h"
-#include <initializer_list>
 
 namespace sn {
 namespace {
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
 {
     constexpr int R = 8;   // rows at a time: their loads are all on their way before the first is used
     const bool mine = (blockIdx.x * THREADS + threadIdx.x) * V < channels;
-    const int c = mine ? (blockIdx.x * THREADS + threadIdx.x) * V : 0;
+    const int c = mine ? min((int)(blockIdx.x * THREADS + threadIdx.x) * V, channels - V) : 0;
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
     if (mine && r0 < r1) {
         Taps<T, V, W> taps;
@@ -147,8 +147,8 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
                                                              const T *__restrict__ dstate_out)
 {
     constexpr int R = W <= 5 ? 8 : 16, H = W - 1;
-    const int c = (blockIdx.x * THREADS + threadIdx.x) * V;
-    if (c >= channels) return;
+    if ((blockIdx.x * THREADS + threadIdx.x) * V >= channels) return;
+    const int c = min((int)(blockIdx.x * THREADS + threadIdx.x) * V, channels - V);
     Taps<T, V, W> taps;
     taps.load(w, bias, c);
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
@@ -380,31 +380,18 @@ int run_of(int64_t rows, int blocks, int least)
     return (int)(run < least ? least : run);
 }
 
-// The channels of a thread: MOST where every tensor's rows can be accessed so many at a time, else 2, else 1.
-template <int MOST, typename F> hipError_t by_vector(int most, F f)
+// The channels of a thread: MOST if there are as many (IN_WHOLE: and no rest), else 1.
+template <int MOST, bool IN_WHOLE, typename F> hipError_t by_vector(int channels, F f)
 {
-    if (most >= MOST) return f(WidthIs<MOST>());
-    if (MOST > 2 && most >= 2) return f(WidthIs<2>());
+    if (channels >= MOST && !(IN_WHOLE && channels % MOST)) return f(WidthIs<MOST>());
     return f(WidthIs<1>());
-}
-
-struct Rows2 {   // a tensor of rows
-    const void *p;
-    int64_t ld;
-};
-int vector_of(int channels, int esize, std::initializer_list<Rows2> tensors)
-{
-    int v = 16 / esize;
-    for (const Rows2 &t : tensors)
-        while (v > 1 && !(rows_aligned(t.p, t.ld, esize, v) && channels % v == 0)) v /= 2;
-    return v;
 }
 
 template <typename T> hipError_t fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off, const void *state_in,
                                      void *state_out, hipStream_t st)
 {
     return by_width(s.width, [&](auto W) {
-        return by_vector<16 / sizeof(T)>(vector_of(s.channels, sizeof(T), {{x, s.ld_x}, {y, s.ld_y}}), [&](auto V) {
+        return by_vector<16 / sizeof(T), false>(s.channels, [&](auto V) {
             const int blocks = div_up(s.channels, V.value * THREADS), run = run_of(s.rows, blocks, 32);
             conv1d_fwd_kernel<T, V.value, W.value><<<dim3(blocks, s.rows ? div_up(s.rows, run) : 1), THREADS, 0, st>>>(
                 (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows_of(s, off), run, (const T *)state_in, (T *)state_out);
@@ -415,7 +402,6 @@ template <typename T> hipError_t fwd(const void *x, const void *w, const float *
 
 constexpr int BWD_V = 4;   // channels of a thread at most: with 8 the windows of x and dp alone would take 176 registers
 
-// Slices do not depend on how a call's tensors are aligned, so that the scratch does not either.
 int bwd_run(int64_t rows, int channels) { return run_of(rows, div_up(channels, BWD_V * THREADS), 64); }   // 64 rows: the turn that fills the windows costs little
 
 template <typename T> hipError_t bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
@@ -424,7 +410,7 @@ template <typename T> hipError_t bwd(const void *x, const void *w, const float *
     return by_width(s.width, [&](auto W) {
         const int run = bwd_run(s.rows, s.channels), slices = s.rows ? div_up(s.rows, run) : 1;
         const SeqRows rows = rows_of(s, off);
-        hipError_t e = by_vector<BWD_V>(vector_of(s.channels, sizeof(T), {{x, s.ld_x}, {dy, s.ld_y}, {dx, s.ld_dx}}), [&](auto V) {
+        hipError_t e = by_vector<BWD_V, false>(s.channels, [&](auto V) {
             conv1d_bwd_kernel<T, V.value, W.value><<<dim3(div_up(s.channels, V.value * THREADS), slices), THREADS, 0, st>>>(
                 (const T *)x, (const T *)w, bias, (const T *)dy, (T *)dx, (float *)scratch, s.channels, s.silu, s.ld_x, s.ld_y, s.ld_dx, rows, run,
                 (const T *)state_in, (const T *)dstate_out);
@@ -444,7 +430,8 @@ template <typename T> hipError_t step(const void *x, const void *w, const float 
                                       const sn_conv1d_shape &s, hipStream_t st)
 {
     return by_width(s.width, [&](auto W) {
-        return by_vector<16 / sizeof(T)>(vector_of(s.channels, sizeof(T), {{x, s.ld_x}, {y, s.ld_y}, {state, s.channels}, {state_out, s.channels}}), [&](auto V) {
+        // a state updated in place must not be read by two threads
+        return by_vector<16 / sizeof(T), true>(s.channels, [&](auto V) {
             conv1d_step_kernel<T, V.value, W.value><<<dim3((int)s.rows, div_up(s.channels, V.value * THREADS)), THREADS, 0, st>>>(
                 (const T *)x, (const T *)w, bias, (T *)y, (const T *)state, (T *)state_out, slots, num_slots, s.channels, s.silu, s.ld_x, s.ld_y);
             return hipGetLastError();

@@ -306,12 +306,12 @@ HeadGrid grid_of(int64_t rows, int q_heads, int k_heads)
 
 template <int V> struct Is { static constexpr int value = V; };
 
-// f(E, NU, LPH): the widest unit that the sizes and the alignment allow
-template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, int aligned, F f)
+// f(E, NU, LPH): the widest unit that the sizes allow
+template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, F f)
 {
     constexpr int most = 16 / (int)sizeof(T);
     int e = most;
-    while (e > 1 && (e > aligned || (rot_dim / 2) % e || (head_dim - rot_dim) % e)) e /= 2;
+    while (e > 1 && ((rot_dim / 2) % e || (head_dim - rot_dim) % e)) e /= 2;
     const int units = rot_dim / 2 / e + (head_dim - rot_dim + 2 * e - 1) / (2 * e);
     const auto pick = [&](auto E) {
         if (units <= 1) return f(E, Is<1>(), Is<1>());
@@ -329,15 +329,6 @@ template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, 
     return pick(Is<1>());
 }
 
-int alignment(const void *p, int64_t ld, int esize)
-{
-    int v = 16 / esize;
-    while (v > 1 && !rows_aligned(p, ld, esize, v)) v /= 2;
-    return v;
-}
-
-int least(int a, int b) { return a < b ? a : b; }
-
 template <typename T, bool BWD>
 hipError_t launch(const void *q, const void *k, const float *wq, const float *wk, const int32_t *pos, const float *freq, const void *gq, const void *gk, void *oq,
                   void *ok, int64_t ld_gq, int64_t ld_gk, int64_t ld_oq, int64_t ld_ok, const sn_headnorm_shape &s, float *part, hipStream_t st)
@@ -345,14 +336,7 @@ hipError_t launch(const void *q, const void *k, const float *wq, const float *wk
     const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads);
     const HeadArgs h = {{{q, gq, oq, wq, s.ld_q, ld_gq, ld_oq, s.q_heads, g.q_parts}, {k, gk, ok, wk, s.ld_k, ld_gk, ld_ok, s.k_heads, g.k_parts}}, pos, freq, part,
                         (int)s.rows, s.head_dim, s.rot_dim, s.interleaved, s.eps};
-    int al = 16 / (int)sizeof(T);
-    for (const HeadSide &side : h.side) {
-        if (!side.heads) continue;
-        al = least(al, least(alignment(side.x, side.ld_x, sizeof(T)), alignment(side.out, side.ld_out, sizeof(T))));
-        if (BWD) al = least(al, alignment(side.g, side.ld_g, sizeof(T)));
-    }
-    while (s.head_dim % al) al /= 2;
-    return by_size<T>(s.head_dim, s.rot_dim, al, [&](auto E, auto NU, auto LPH) {
+    return by_size<T>(s.head_dim, s.rot_dim, [&](auto E, auto NU, auto LPH) {
         headnorm_kernel<T, E.value, NU.value, LPH.value, BWD><<<dim3(g.blocks, g.q_parts + g.k_parts), THREADS, 0, st>>>(h);
         return hipGetLastError();
     });

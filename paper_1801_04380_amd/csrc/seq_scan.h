@@ -188,16 +188,16 @@ __device__ inline float keep_if(bool here, float v) { return __uint_as_float(__f
 __device__ inline float pick(uint32_t mask, float a, float b) { return __uint_as_float((__float_as_uint(a) & mask) | (__float_as_uint(b) & ~mask)); }
 
 // VE neighbouring channels of a row, as they lie in memory: of the nch channels that a row of the tile at `tile` begins with (the place of its
-// first row, the same for all lanes: the lane's part of an address is 32 bits) those from co on.  WHOLE: in pieces (then a thread's channels
-// are all there or none is); otherwise one by one.
-template <typename T, int NL, bool WHOLE> struct Staged {
-    static constexpr int VE = ScanGeo<NL>::VE, P = WHOLE ? ScanGeo<NL>::template piece<T>() : 1, PN = VE / P;
+// first row, the same for all lanes: the lane's part of an address is 32 bits) those from co on.  WIDE 2, 1, 0: in pieces of up to
+// 16 bytes, by twos (a piece's channels are all there or none is), one by one.
+template <typename T, int NL, int WIDE> struct Staged {
+    static constexpr int VE = ScanGeo<NL>::VE, P = WIDE == 2 ? ScanGeo<NL>::template piece<T>() : WIDE && VE > 1 ? 2 : 1, PN = VE / P;
     Pack<T, P> p[PN];
     __device__ void load(const char *tile, uint32_t ld, int row, int co, int nch)
     {
 #pragma unroll
         for (int i = 0; i < PN; ++i) {
-            const int c = WHOLE ? (co < nch ? co + i * P : 0) : min(co + i, nch - 1);
+            const int c = WIDE ? (co + i * P < nch ? co + i * P : 0) : min(co + i, nch - 1);
             p[i].load(reinterpret_cast<const T *>(tile + (uint32_t)(row * ld + c * (uint32_t)sizeof(T))));
         }
     }
@@ -211,11 +211,11 @@ template <typename T, int NL, bool WHOLE> struct Staged {
     __device__ void set(int i, float v) { p[i / P].set(i % P, v); }
 };
 
-// The rows of B and C of one group, NP values each, a thread's share of a tile of which the first `have` rows are in the tensors.  WHOLE: four
+// The rows of B and C of one group, NP values each, a thread's share of a tile of which the first `have` rows are in the tensors.  WIDE: four
 // neighbouring states at a time, so that a wave or two load what all four would one by one.  first .. last - 1: the rows of the piece, the
 // others are staged as zeros.
-template <typename T, int NL, int ROWS, bool BOTH, bool WHOLE> struct StagedBC {
-    static constexpr int NP = ScanGeo<NL>::NP, V = WHOLE ? 4 : 1, EACH = ROWS * NP / V, COUNT = (BOTH ? 2 : 1) * EACH, PER = (COUNT + 255) / 256;
+template <typename T, int NL, int ROWS, bool BOTH, int WIDE> struct StagedBC {
+    static constexpr int NP = ScanGeo<NL>::NP, V = WIDE ? 4 : 1, EACH = ROWS * NP / V, COUNT = (BOTH ? 2 : 1) * EACH, PER = (COUNT + 255) / 256;
     Pack<T, V> v[PER];
     // B, C: the tile's first rows; the first alone unless BOTH
     __device__ void load(const char *B, uint32_t ld_b, const char *C, uint32_t ld_c, int have, int N)
@@ -223,7 +223,7 @@ template <typename T, int NL, int ROWS, bool BOTH, bool WHOLE> struct StagedBC {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int k = i * 256 + threadIdx.x, r = min(k % EACH * V / NP, have - 1), n = k * V % NP;
-            const uint32_t at = (uint32_t)(WHOLE ? (n < N ? n : 0) : min(n, N - 1)) * (uint32_t)sizeof(T);
+            const uint32_t at = (uint32_t)(WIDE ? (n < N ? n : 0) : min(n, N - 1)) * (uint32_t)sizeof(T);
             v[i].load(reinterpret_cast<const T *>(BOTH && k / EACH % 2 ? C + (uint32_t)(r * ld_c + at) : B + (uint32_t)(r * ld_b + at)));
         }
     }
@@ -235,7 +235,7 @@ template <typename T, int NL, int ROWS, bool BOTH, bool WHOLE> struct StagedBC {
             if (k >= COUNT) continue;
             float *to = (BOTH && k >= EACH ? s_C : s_B) + w * V;
             const bool here = r >= first && r < last;
-            if (WHOLE) {
+            if (WIDE) {
                 const bool in = here && n < N;
                 *reinterpret_cast<float4 *>(to) = make_float4(keep_if(in, v[i].get(0)), keep_if(in, v[i].get(V > 1 ? 1 : 0)), keep_if(in, v[i].get(V > 1 ? 2 : 0)), keep_if(in, v[i].get(V > 1 ? 3 : 0)));
             } else {
@@ -256,16 +256,25 @@ int scan_parts_wanted(const sn_scan_shape &s, bool bwd);
 size_t scan_carry_bytes(const sn_scan_shape &s, const ScanPlan &p);
 ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off, const void *u, const void *dt, const float *A, const void *B, const void *C,
                    const float *D, const void *z, const float *bias);
-bool scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan);
-bool scan_whole_states(const void *p, int64_t ld, const sn_scan_shape &s);
+int scan_wide(const sn_scan_shape &s, const ScanPlan &plan);
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws);
-hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st);   // a.states from the inputs
+hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, int wide, hipStream_t st);   // a.states from the inputs
 hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st);
 
 template <int V> struct ScanInt { static constexpr int value = V; };
 template <typename F> hipError_t by_lanes(int NL, F f)
 {
     return NL == 2 ? f(ScanInt<2>()) : NL == 4 ? f(ScanInt<4>()) : NL == 8 ? f(ScanInt<8>()) : f(ScanInt<16>());
+}
+// f(lanes of a channel, width): with eight lanes and more a thread stages two channels at most, and twos are whole pieces
+template <typename F> hipError_t by_lanes_and_width(int NL, int wide, F f)
+{
+    return by_lanes(NL, [&](auto L) {
+        if (wide == 2) return f(L, ScanInt<2>());
+        if constexpr (L.value < 8)
+            if (wide == 1) return f(L, ScanInt<1>());
+        return f(L, ScanInt<0>());
+    });
 }
 
 }  // namespace sn

@@ -16,7 +16,7 @@ constexpr int THREADS = 256;
 
 // MODE 0: y (and, if asked for, the states of tiles and the final states); 1: the chunk's final state from zero and the sum of delta;
 // 2: the states of tiles alone.
-template <typename T, int NL, bool WHOLE, int MODE>
+template <typename T, int NL, int WIDE, int MODE>
 __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, LOCAL ? r1 - 1 : r0);   // a chunk hands on the state of the sequence that holds its last row
         Piece next = piece_from<ROWS>(a.rows, at, LOCAL ? max(r0, at.begin) : r0, r0, r1);
-        Staged<T, NL, WHOLE> u[RP], dt[RP], z[RP];
-        StagedBC<T, NL, ROWS, OUT, WHOLE> BC;
+        Staged<T, NL, WIDE> u[RP], dt[RP], z[RP];
+        StagedBC<T, NL, ROWS, OUT, WIDE> BC;
         const auto fetch = [&]() {
             const int64_t t0 = next.t0;
             const int have = a.rows.rows - next.t0;   // rows of the tensors from there on
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
             }
             if (OUT && a.hT && now.end) lane.store(a.hT, now.seq, a, h);
             __syncthreads();
-            Staged<T, NL, WHOLE> y[RP];
+            Staged<T, NL, WIDE> y[RP];
             if (OUT)
 #pragma unroll
                 for (int j = 0; j < RP; ++j)
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a, int reverse)
 }
 
 // One token: a thread holds four states of a channel, NL neighbouring threads a channel.  Bound by reading and writing the states.  WHOLE: a
-// thread's four are there and aligned, in the states, in A and in the rows of B and C.
+// thread's four are all there, or none is.
 template <typename T, int NL, bool WHOLE>
 __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const float *state, float *state_out, const int32_t *slots, int num_slots)
 {
@@ -239,8 +239,14 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     Pack<T, 4> b, cc;
     if (WHOLE) {
         const int n = n0 < a.N ? n0 : 0;
-        *reinterpret_cast<float4 *>(h) = *reinterpret_cast<const float4 *>(from + n);
-        *reinterpret_cast<float4 *>(A4) = *reinterpret_cast<const float4 *>(A + n);
+        Pack<float, 4> h4, a4;
+        h4.load(from + n);
+        a4.load(A + n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[i] = h4.e[i];
+            A4[i] = a4.e[i];
+        }
         b.load(B + n);
         cc.load(C + n);
     } else {
@@ -265,7 +271,10 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
         if (n0 + i < a.N) sum = fmaf(h[i], cc.get(i), sum);
     }
     if (WHOLE) {
-        if (n0 < a.N) *reinterpret_cast<float4 *>(to + n0) = make_float4(h[0], h[1], h[2], h[3]);
+        Pack<float, 4> h4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h4.e[i] = h[i];
+        if (n0 < a.N) h4.store(to + n0);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -279,17 +288,12 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     seq_st((T *)((char *)a.y + t * a.ld_y) + c, y);
 }
 
-template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st)
+template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, int wide, hipStream_t st)
 {
-    return by_lanes(p.NL, [&](auto NL) {
+    return by_lanes_and_width(p.NL, wide, [&](auto NL, auto WIDE) {
         const dim3 grid(p.chunks, p.blocks);
-        if (s.dtype == SN_BF16) {
-            if (whole) scan_fwd_kernel<bf16_t, NL.value, true, MODE><<<grid, THREADS, 0, st>>>(a);
-            else scan_fwd_kernel<bf16_t, NL.value, false, MODE><<<grid, THREADS, 0, st>>>(a);
-        } else {
-            if (whole) scan_fwd_kernel<float, NL.value, true, MODE><<<grid, THREADS, 0, st>>>(a);
-            else scan_fwd_kernel<float, NL.value, false, MODE><<<grid, THREADS, 0, st>>>(a);
-        }
+        if (s.dtype == SN_BF16) scan_fwd_kernel<bf16_t, NL.value, WIDE.value, MODE><<<grid, THREADS, 0, st>>>(a);
+        else scan_fwd_kernel<float, NL.value, WIDE.value, MODE><<<grid, THREADS, 0, st>>>(a);
         return hipGetLastError();
     });
 }
@@ -356,17 +360,12 @@ ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off
     return a;
 }
 
-// Whether the rows of a tensor can be staged in whole pieces: by its address, its stride and the channels of a group.
-bool scan_whole_rows(const void *p, int64_t ld, const sn_scan_shape &s, const ScanPlan &plan)
+// How rows can be staged: by the channels of a group, with four states of B and C at a time where these are whole fours.  Forward and backward over
+// 3 x 517 rows in fp32, 8 states, us of the four kernels: 204 channels in two groups one by one 84, by twos 61, 208 channels by fours 57.
+int scan_wide(const sn_scan_shape &s, const ScanPlan &plan)
 {
-    const int e = s.dtype == SN_BF16 ? 2 : 4, ve = plan.CB / 16, piece = ve * e > 16 ? 16 / e : ve;
-    return rows_aligned(p, s.rows > 1 ? ld : 0, e, piece) && s.channels / s.groups % ve == 0;
-}
-
-// Whether the rows of B or C can be staged four states at a time.
-bool scan_whole_states(const void *p, int64_t ld, const sn_scan_shape &s)
-{
-    return s.states % 4 == 0 && rows_aligned(p, s.rows > 1 ? ld : 0, s.dtype == SN_BF16 ? 2 : 4, 4);
+    const int e = s.dtype == SN_BF16 ? 2 : 4, ve = plan.CB / 16, piece = ve * e > 16 ? 16 / e : ve, channels = s.channels / s.groups;
+    return s.states % 4 ? 0 : channels % piece == 0 ? 2 : channels % 2 == 0 ? 1 : 0;
 }
 
 void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void *ws)
@@ -393,17 +392,17 @@ hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse,
     return hipGetLastError();
 }
 
-template <int MODE> static hipError_t fwd_in_chunks(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st)
+template <int MODE> static hipError_t fwd_in_chunks(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, int wide, hipStream_t st)
 {
     if (p.parts > 1) {
-        hipError_t e = launch_fwd<1>(a, s, p, whole, st);
+        hipError_t e = launch_fwd<1>(a, s, p, wide, st);
         if (e == hipSuccess) e = launch_scan_carry(a, p, false, st);
         if (e != hipSuccess) return e;
     }
-    return launch_fwd<MODE>(a, s, p, whole, st);
+    return launch_fwd<MODE>(a, s, p, wide, st);
 }
 
-hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, bool whole, hipStream_t st) { return fwd_in_chunks<2>(a, s, p, whole, st); }
+hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, int wide, hipStream_t st) { return fwd_in_chunks<2>(a, s, p, wide, st); }
 
 hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
                            const sn_scan_shape &s, const int32_t *off, const float *h0, float *hT, float *states, void *ws, size_t ws_bytes, hipStream_t st)
@@ -412,10 +411,9 @@ hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const 
     while (p.parts > 1 && scan_carry_bytes(s, p) > ws_bytes) p = scan_plan(s, p.parts - 1);
     ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
     a.y = y; a.h0 = h0; a.hT = hT; a.states = states;
-    const bool whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && scan_whole_rows(y, s.ld_y, s, p) &&
-                       (!z || scan_whole_rows(z, s.ld_z, s, p)) && scan_whole_states(B, s.ld_b, s) && scan_whole_states(C, s.ld_c, s);
+    const int wide = scan_wide(s, p);
     if (p.parts > 1) scan_set_carry(a, s, p, ws);
-    return fwd_in_chunks<0>(a, s, p, whole, st);
+    return fwd_in_chunks<0>(a, s, p, wide, st);
 }
 
 hipError_t launch_scan_step(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
@@ -425,9 +423,7 @@ hipError_t launch_scan_step(const void *u, const void *dt, const float *A, const
     ScanArgs a = scan_args(s, p, nullptr, u, dt, A, B, C, D, z, bias);
     a.y = y;
     const dim3 grid((int)s.rows, div_up((int64_t)s.channels * p.NL, THREADS));
-    const int e = s.dtype == SN_BF16 ? 2 : 4;
-    const bool whole = s.states % 4 == 0 && rows_aligned(state, 0, 4, 4) && rows_aligned(state_out, 0, 4, 4) && rows_aligned(A, 0, 4, 4) &&
-                       rows_aligned(B, s.rows > 1 ? s.ld_b : 0, e, 4) && rows_aligned(C, s.rows > 1 ? s.ld_c : 0, e, 4);
+    const bool whole = s.states % 4 == 0;
     return by_lanes(p.NL, [&](auto NL) {
         if (s.dtype == SN_BF16) {
             if (whole) scan_step_kernel<bf16_t, NL.value, true><<<grid, THREADS, 0, st>>>(a, state, state_out, slots, num_slots);

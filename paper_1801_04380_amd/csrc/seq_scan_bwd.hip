@@ -27,7 +27,7 @@ struct RowIn {
 };
 
 // What of the gradient of the states a chunk hands on to the one before it, starting from zero, and its sum of delta.
-template <typename T, int NL, bool WHOLE>
+template <typename T, int NL, int WIDE>
 __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
@@ -48,8 +48,8 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     bool crossed = false;
     SeqAt at = seq_find(a.rows, r0);   // a chunk hands on the gradient of the sequence that holds its first row
     Piece next = piece_before<TS>(a.rows, at, min(r1, at.end), r0);
-    Staged<T, NL, WHOLE> dt, z, dy;
-    StagedBC<T, NL, TS, false, WHOLE> C;
+    Staged<T, NL, WIDE> dt, z, dy;
+    StagedBC<T, NL, TS, false, WIDE> C;
     const char *pdt = (const char *)a.dt + c0 * sizeof(T), *pz = (const char *)a.z + c0 * sizeof(T), *pdy = (const char *)a.dy + c0 * sizeof(T);
     const char *pC = (const char *)a.C + group * a.N * sizeof(T);
     const uint32_t is_softplus = a.softplus ? ~0u : 0u, is_gate = a.gate ? ~0u : 0u;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(THREADS) scan_bwd_local_kernel(ScanArgs a)
     if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
 }
 
-template <typename T, int NL, bool WHOLE>
+template <typename T, int NL, int WIDE>
 __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
 {
     using G = ScanGeo<NL>;
@@ -156,8 +156,8 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, r1 - 1);
         Piece next = piece_before<TS>(a.rows, at, r1, r0);
-        Staged<T, NL, WHOLE> u, dt, z, dy;
-        StagedBC<T, NL, TS, true, WHOLE> BC;
+        Staged<T, NL, WIDE> u, dt, z, dy;
+        StagedBC<T, NL, TS, true, WIDE> BC;
         float4 kept = {};   // the state in front of the piece's tile
         const auto fetch = [&]() {
             const int64_t t0 = next.t0;
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
             if (a.dh0 && now.start) lane.store(a.dh0, now.seq, a, g);
             __syncthreads();
             const bool in = now.holds(now.t0 + row);
-            Staged<T, NL, WHOLE> du, ddt, dz;
+            Staged<T, NL, WIDE> du, ddt, dz;
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 const float vb = s_x[row][co + i], va = s_qa[row][co + i] * 0.69314718055994530942f /* A is A2 * ln 2 */, gy = s_g[row][co + i];
@@ -411,16 +411,16 @@ __global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunk
     to[at] = sum;
 }
 
-template <typename T, int NL, bool WHOLE> hipError_t bwd_in_chunks(const ScanArgs &a, const ScanPlan &p, hipStream_t st)
+template <typename T, int NL, int WIDE> hipError_t bwd_in_chunks(const ScanArgs &a, const ScanPlan &p, hipStream_t st)
 {
     const dim3 grid(p.chunks, p.blocks);
     if (p.parts > 1) {
-        scan_bwd_local_kernel<T, NL, WHOLE><<<grid, THREADS, 0, st>>>(a);
+        scan_bwd_local_kernel<T, NL, WIDE><<<grid, THREADS, 0, st>>>(a);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess) e = launch_scan_carry(a, p, true, st);
         if (e != hipSuccess) return e;
     }
-    scan_bwd_kernel<T, NL, WHOLE><<<grid, THREADS, 0, st>>>(a);
+    scan_bwd_kernel<T, NL, WIDE><<<grid, THREADS, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -457,10 +457,7 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
     a.h0 = h0;
     a.dy = g.dy; a.du = g.du; a.ddt = g.ddt; a.dB = g.dB; a.dC = g.dC; a.dz = g.dz; a.dhT = g.dhT; a.dh0 = g.dh0;
-    const bool in_whole = scan_whole_rows(u, s.ld_u, s, p) && scan_whole_rows(dt, s.ld_dt, s, p) && (!z || scan_whole_rows(z, s.ld_z, s, p)) &&
-                          scan_whole_states(B, s.ld_b, s) && scan_whole_states(C, s.ld_c, s);
-    const bool whole = in_whole && scan_whole_rows(g.dy, s.ld_y, s, p) && scan_whole_rows(g.du, s.ld_du, s, p) && scan_whole_rows(g.ddt, s.ld_ddt, s, p) &&
-                       (!z || scan_whole_rows(g.dz, s.ld_dz, s, p));
+    const int wide = scan_wide(s, p);
     char *at = (char *)ws;
     a.states = states ? const_cast<float *>(states) : (float *)at;
     at += replay;
@@ -471,12 +468,11 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     a.part_bias = (float *)at; at += b.d;
     a.part_bc = (float *)at;
     hipError_t e = hipSuccess;
-    if (!states && s.rows) e = launch_scan_states(a, s, p, in_whole, st);
+    if (!states && s.rows) e = launch_scan_states(a, s, p, wide, st);
     if (e != hipSuccess) return e;
     const bool bf16 = s.dtype == SN_BF16;
-    e = by_lanes(p.NL, [&](auto NL) {
-        if (bf16) return whole ? bwd_in_chunks<bf16_t, NL.value, true>(a, p, st) : bwd_in_chunks<bf16_t, NL.value, false>(a, p, st);
-        return whole ? bwd_in_chunks<float, NL.value, true>(a, p, st) : bwd_in_chunks<float, NL.value, false>(a, p, st);
+    e = by_lanes_and_width(p.NL, wide, [&](auto NL, auto WIDE) {
+        return bf16 ? bwd_in_chunks<bf16_t, NL.value, WIDE.value>(a, p, st) : bwd_in_chunks<float, NL.value, WIDE.value>(a, p, st);
     });
     if (e != hipSuccess) return e;
     if (s.rows) {

@@ -352,6 +352,42 @@ def test_nan_of_one_sequence_stays_in_it():
     close(g["dh0"][[0, 2]], want["dh0"][[0, 2]])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,N,G", [(132, 8, 1), (138, 8, 1), (204, 8, 2), (70, 16, 1), (66, 12, 1), (2, 4, 1), (6, 32, 1), (129, 8, 1)])
+def test_scan_widths(dtype, D, N, G):
+    """Channels of a group in whole pieces, by twos and one by one, the last block of channels with less than a thread's; rows at any alignment."""
+    lengths = [21, 0, 40]
+    c = Scan(dtype, lengths, 63, D, N, G, D + N)
+    kw, shape = {"seqs": 3, "offsets": offsets(lengths)}, c.shape(True)
+    y, hT, want = c.want()
+    gy, gh = c.forward(kw, None, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_FWD)[1]))
+    gy.check(y)
+    close(gh, hT)
+    c.check(c.backward(kw, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_BWD)[1] + sn.sn_scan_states_bytes(shape))), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 7, 9, 2047, 2049])
+def test_conv1d_channels_of_no_whole_vector(dtype, D):
+    lengths, used, rows, kw = layout("ragged_tail")
+    d, S, W = Data(dtype, D), len(lengths), 4
+    x, w, dy, bias = d.normal(rows, D), d.normal(D, W, scale=0.5), d.normal(rows, D), d.normal(D, dtype=torch.float32)
+    state, dstate = d.normal(S, W - 1, D), d.normal(S, W - 1, D)
+    y, dx = Out(rows, D, d.dtype, 3, 1, used), Out(rows, D, d.dtype, 3, 1, used)
+    out, din, dw, db = torch.empty_like(state).cuda(), torch.empty_like(state).cuda(), torch.empty(D, W, device="cuda"), torch.empty(D, device="cuda")
+    xg, dyg = strided(x, 1, 1), strided(dy, 2, 3)
+    sn.sn_causal_conv1d_fwd(xg, w.cuda(), bias.cuda(), y.t, state_in=state.cuda(), state_out=out, **kw)
+    sn.sn_causal_conv1d_bwd(xg, w.cuda(), bias.cuda(), dyg, dx.t, dw, db, bytes_(sn.sn_causal_conv1d_scratch_bytes(rows, D, W)), state_in=state.cuda(),
+                            dstate_out=dstate.cuda(), dstate_in=din, **kw)
+    wy, wout = oracle.conv1d_fwd(f64(x)[:used], f64(w), f64(bias), lengths, f64(state))
+    wdx, wdw, wdb, wdin = oracle.conv1d_bwd(f64(x)[:used], f64(w), f64(bias), f64(dy)[:used], lengths, f64(state), f64(dstate))
+    y.check(wy)
+    dx.check(wdx)
+    assert np.array_equal(f64(out), wout)
+    for got, want, t in ((dw, wdw, torch.float32), (db, wdb, torch.float32), (din, wdin, d.dtype)):
+        close(got, want, t)
+
+
 @pytest.mark.parametrize("dtype,S,L,N", [("bf16", 300, 4, 16), ("f32", 41, 16, 8), ("f32", 90, 1, 32), ("bf16", 23, 15, 5)])
 def test_scan_of_many_short_sequences_of_equal_length(dtype, S, L, N):
     """They share tiles and chunks; as ragged sequences and as equal ones the rows are cut in the same way, so the results are the same."""
