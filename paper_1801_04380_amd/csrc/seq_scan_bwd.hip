@@ -370,28 +370,33 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
         });
 }
 
-// dB and dC from the sums of the channel blocks: one thread per row, group, tensor and state.
-template <typename T>
-__global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int groups, int NP)
+// dB and dC from the sums of the channel blocks: one thread per row, group, tensor and state, k counts them.
+template <typename T> __device__ inline void join_bc(const ScanArgs &a, int groups, int64_t k)
 {
-    const int64_t k = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * THREADS + threadIdx.x;
-    const int n = (int)(k % NP), which = (int)(k / NP % 2), group = (int)(k / (2 * NP) % groups);
-    const int64_t row = k / (2 * NP) / groups;
+    const int n = (int)(k % a.NP), which = (int)(k / a.NP % 2), group = (int)(k / (2 * a.NP) % groups);
+    const int64_t row = k / (2 * a.NP) / groups;
     if (row >= a.rows.rows || n >= a.N) return;
     if (a.rows.off && !seq_find(a.rows, (int)row).holds((int)row, a.rows)) return;
     float sum = 0.f;
     for (int b = 0; b < a.blocks_per_group; ++b)
-        sum += a.part_bc[(((int64_t)group * a.blocks_per_group + b) * a.rows.rows + row) * (2 * NP) + which * NP + n];
+        sum += a.part_bc[(((int64_t)group * a.blocks_per_group + b) * a.rows.rows + row) * (2 * a.NP) + which * a.NP + n];
     char *to = which ? (char *)a.dC + row * a.ld_dc : (char *)a.dB + row * a.ld_db;
     seq_st((T *)to + group * a.N + n, sum);
 }
 
-// dA, dD and the bias's gradient from the sums of the chunks: 16 threads along the chunks of each value, joined in a fixed order.
-__global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunks, float *__restrict__ dA, float *__restrict__ dD, float *__restrict__ dbias)
+// What is left to join, in one launch: the first `sums` workgroups take dA, dD and the bias's gradient from the sums of the chunks, 16 threads
+// along the chunks of each value, joined in a fixed order; the others dB and dC.
+template <typename T>
+__global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int groups, int chunks, unsigned sums, float *__restrict__ dA, float *__restrict__ dD, float *__restrict__ dbias)
 {
-    __shared__ float sums[16][16];
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (block >= sums) {
+        join_bc<T>(a, groups, (block - sums) * THREADS + threadIdx.x);
+        return;
+    }
+    __shared__ float lds[16][16];
     const int lane = threadIdx.x / 16;
-    const int64_t i = (int64_t)blockIdx.x * 16 + threadIdx.x % 16, each = (int64_t)a.channels * a.N;
+    const int64_t i = block * 16 + threadIdx.x % 16, each = (int64_t)a.channels * a.N;
     const float *from = a.part_a;
     float *to = nullptr;
     int64_t at = 0, stride = a.channels;
@@ -402,12 +407,12 @@ __global__ void __launch_bounds__(THREADS) scan_sum_kernel(ScanArgs a, int chunk
     if (to)
 #pragma unroll 8
         for (int c = lane; c < chunks; c += 16) sum += from[c * stride + at];
-    sums[lane][threadIdx.x % 16] = sum;
+    lds[lane][threadIdx.x % 16] = sum;
     __syncthreads();
     if (lane || !to) return;
     sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < 16; ++c) sum += sums[c][threadIdx.x];
+    for (int c = 0; c < 16; ++c) sum += lds[c][threadIdx.x];
     to[at] = sum;
 }
 
@@ -475,17 +480,11 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
         return bf16 ? bwd_in_chunks<bf16_t, NL.value, WIDE.value>(a, p, st) : bwd_in_chunks<float, NL.value, WIDE.value>(a, p, st);
     });
     if (e != hipSuccess) return e;
-    if (s.rows) {
-        const int64_t n = s.rows * s.groups * 8 * p.NL;
-        const int64_t all = (n + THREADS - 1) / THREADS, most = 1 << 20;   // in x: a dimension of a grid has to stay below 2^32 threads
-        const dim3 blocks((unsigned)(all < most ? all : most), (unsigned)((all + most - 1) / most));
-        if (bf16) scan_join_kernel<bf16_t><<<blocks, THREADS, 0, st>>>(a, s.groups, 4 * p.NL);
-        else scan_join_kernel<float><<<blocks, THREADS, 0, st>>>(a, s.groups, 4 * p.NL);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    const int64_t n = (int64_t)s.channels * (s.states + 2);
-    scan_sum_kernel<<<(unsigned)((n + 15) / 16), THREADS, 0, st>>>(a, p.chunks, g.dA, g.dD, g.ddt_bias);
+    const int64_t sums = ((int64_t)s.channels * (s.states + 2) + 15) / 16, all = sums + (s.rows * s.groups * 8 * p.NL + THREADS - 1) / THREADS;
+    const int64_t most = 1 << 20;   // in x: a dimension of a grid has to stay below 2^32 threads
+    const dim3 blocks((unsigned)(all < most ? all : most), (unsigned)((all + most - 1) / most));
+    if (bf16) scan_join_kernel<bf16_t><<<blocks, THREADS, 0, st>>>(a, s.groups, p.chunks, (unsigned)sums, g.dA, g.dD, g.ddt_bias);
+    else scan_join_kernel<float><<<blocks, THREADS, 0, st>>>(a, s.groups, p.chunks, (unsigned)sums, g.dA, g.dD, g.ddt_bias);
     return hipGetLastError();
 }
 
