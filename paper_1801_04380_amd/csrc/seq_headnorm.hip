@@ -5,7 +5,8 @@
 // nothing; behind rot_dim a unit is 2 E neighbours that are not turned.  LPH lanes (a power of two) hold a head, a wave 64 / LPH
 // heads of one row at a time, NU units a lane.  The wave then takes the row's next heads, loading them before it works on these.  A workgroup
 // has to do with q or with k alone, whose weight its lanes hold.  A row's angles are formed once, one by each lane, in 64 bits, and handed
-// round through LDS.
+// round through LDS.  16384 rows, 32 and 8 heads of 128, bf16: forward 60 us (5.6 TB/s, part of it from the memory-side cache), backward
+// 108 us (4.7 TB/s); 32 rows, 16 and 4 heads of 64: 4.2 us.
 #include "seq.h"
 #include <type_traits>
 

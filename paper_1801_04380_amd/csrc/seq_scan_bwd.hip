@@ -5,10 +5,13 @@
 // and everything else is made of it and of the states h:
 //   du = gy D + delta sum_n g B        ddelta = u sum_n g B + sum_n A q,  q = g exp(delta A) h[t-1]        dA = sum_t delta q
 //   dB = sum_d g delta u               dC = sum_d gy h
-// A tile's states are computed again from the one kept before it (16 rows of states and decays in registers, four states a lane),
+// A tile's states are computed again from the one kept before it (eight rows of states and decays in registers at a time, four states a lane),
 // then the tile is walked backwards.  Three sums over a channel's states and two over a group's channels per row come on top of the
 // products: scatter_sum shares an exchange among as many values as it has lanes, 8 values a row and lane for dB and dC.  The sums of a
-// workgroup's channels go to the workspace and are joined by scan_join_kernel, in a fixed order.  Bound by the vector units.
+// workgroup's channels go to the workspace and are joined by scan_join_kernel, in a fixed order.  Bound by the vector units: 104 instructions a row
+// and wave, of which 60 are the formulas' for four states, and busy in 84 % of the cycles at two waves a SIMD (registers; four waves spill
+// and are slower).  16384 x 2048 x 16: 492 us.  All 16 rows' states in registers at a time instead of eight, of which the second half's
+// are computed from the state between the halves: slower, at one wave a SIMD.
 // Cut into chunks like the forward pass where channels and sequences do not fill the chip: scan_bwd_local_kernel takes what a chunk hands to
 // the one before it, scan_carry_kernel joins.
 #include "seq_scan.h"
