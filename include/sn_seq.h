@@ -10,8 +10,8 @@
  *    element; everything else is fp32 (or int32) and aligned to 4 bytes; workspaces are 256-byte aligned.
  *  - Sequences lie packed one behind the other.  seq_offsets == NULL: `seqs` sequences of rows / seqs rows each
  *    (seqs must divide rows).  Otherwise int32[seqs + 1] in device memory, ascending: sequence s is the rows
- *    seq_offsets[s] .. seq_offsets[s+1] - 1.  Empty sequences are allowed.  Rows that no sequence holds (behind the last) are
- *    neither read for any result nor written.  Offsets that descend, or leave 0 .. rows, give undefined results, but no access
+ *    seq_offsets[s] .. seq_offsets[s+1] - 1.  Empty sequences are allowed.  Rows that no sequence holds (behind the last, in
+ *    front of the first) are neither read for any result nor written.  Offsets that descend, or leave 0 .. rows, give undefined results, but no access
  *    outside the tensors.
  *  - Sizes, SN_ERR_UNSUPPORTED beyond: rows 2^30 (of a step call 2^24 - 1), sequences 2^24 - 1, channels of the convolution 65535 * 256,
  *    channels of the scan 65535 blocks of 16 of one group.  Addresses are 64-bit.  rows = 0 is a valid call.

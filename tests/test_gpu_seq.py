@@ -419,6 +419,54 @@ def test_scan_of_many_sequences_most_of_them_empty():
     c.check(c.backward(kw, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_BWD)[1] + sn.sn_scan_states_bytes(shape))), want)
 
 
+def test_conv1d_of_many_sequences_most_of_them_empty():
+    lengths = [0] * 70 + [19] + [0] * 131 + [1] + [0] * 64 + [2] + [0] * 3
+    d, S, W, D = Data("bf16", 3), len(lengths), 4, 300
+    x, w, state = d.normal(22, D), d.normal(D, W, scale=0.5), d.normal(S, W - 1, D)
+    y, out = Out(22, D, d.dtype), torch.full_like(state, SENTINEL).cuda()
+    sn.sn_causal_conv1d_fwd(x.cuda(), w.cuda(), None, y.t, offsets=offsets(lengths), seqs=S, state_in=state.cuda(), state_out=out)
+    want, end = oracle.conv1d_fwd(f64(x), f64(w), None, lengths, f64(state))
+    y.check(want)
+    assert np.array_equal(f64(out), end)
+
+
+@pytest.mark.parametrize("front", [3, 40])
+def test_rows_in_front_of_the_first_sequence(front):
+    """They are as those behind the last: the results are those of the rows from there on, and nothing else is written."""
+    lengths, N, E = [0, 25, 9], 8, 24
+    used, off = 34, offsets([0, 25, 9])
+    c = Scan("f32", lengths, used, E, N, 1, front)
+    y, hT, want = c.want()
+    nan = lambda t: torch.cat([torch.full((front, t.shape[1]), float("nan"), device="cuda"), t, torch.full((2, t.shape[1]), float("nan"), device="cuda")])  # noqa: E731
+    c.args = [nan(a) if a is not None and k in ("u", "dt", "B", "C", "z") else a for k, a in zip(c.t, c.args)]
+    c.dy = nan(c.dy.cuda()).cpu()
+    c.rows = c.used = front + used + 2
+    kw, shape = {"seqs": 3, "offsets": off + front}, c.shape(True)
+    gy, gh = c.forward(kw, None, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_FWD)[1]))
+    g = c.backward(kw, bytes_(sn.sn_scan_workspace_query(shape, sn.SN_SCAN_BWD)[1] + sn.sn_scan_states_bytes(shape)))
+    close(gh, hT)
+    got = {"y": gy, **g}
+    for k, v in got.items():
+        right = y if k == "y" else want[k]
+        if isinstance(v, Out):
+            rows = f64(v.t)
+            close(rows[front:front + used], right)
+            assert (rows[:front] == SENTINEL).all() and (rows[front + used:] == SENTINEL).all(), k
+        else:
+            close(v, right)
+    d = Data("f32", 4)
+    x, w, dy = d.normal(used, E), d.normal(E, 4, scale=0.5), d.normal(used, E)
+    out, dx, dw = Out(c.rows, E, d.dtype), Out(c.rows, E, d.dtype), torch.empty(E, 4, device="cuda")
+    sn.sn_causal_conv1d_fwd(nan(x.cuda()), w.cuda(), None, out.t, **kw)
+    sn.sn_causal_conv1d_bwd(nan(x.cuda()), w.cuda(), None, nan(dy.cuda()), dx.t, dw, None, bytes_(sn.sn_causal_conv1d_scratch_bytes(c.rows, E, 4)), **kw)
+    wdx, wdw, _, _ = oracle.conv1d_bwd(f64(x), f64(w), None, f64(dy), lengths)
+    close(dw, wdw)
+    for o, right in ((out, oracle.conv1d_fwd(f64(x), f64(w), None, lengths)[0]), (dx, wdx)):
+        rows = f64(o.t)
+        close(rows[front:front + used], right)
+        assert (rows[:front] == SENTINEL).all() and (rows[front + used:] == SENTINEL).all()
+
+
 def test_scan_states_that_grow_or_vanish_at_once():
     """A > 0: a chunk's factor leaves the range while the state is still zero, as nothing has come in.  A = -inf: nothing is kept from one
     token to the next, also where a sequence ends inside a tile.  The answers are whole numbers."""
