@@ -78,9 +78,10 @@ def _call(name, *args):
 # The checks are the larger part of what a small call costs the host: one look at each attribute, messages only when something is wrong.
 def _device(t, what):
     """-> the current device, on which t has to live."""
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    device = t.get_device()   # below 0: not on a GPU
+    if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError("%s: expected a tensor on the current device" % what)
-    return t.get_device()
+    return device
 
 
 def _stream_of(device):
