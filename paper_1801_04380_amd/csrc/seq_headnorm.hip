@@ -307,13 +307,15 @@ HeadGrid grid_of(int64_t rows, int q_heads, int k_heads)
 
 template <int V> struct Is { static constexpr int value = V; };
 
-// f(E, NU, LPH): the widest unit that the sizes allow
-template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, F f)
+// f(E, NU, LPH): the widest unit that the sizes allow, or a narrower one where a row's heads would leave half of a wave's lanes without work
+// (4099 rows, 8 and 8 heads of 16 in fp32, us forward and backward: units of 8 elements 7.4, 12.9, of 2 5.9, 7.6)
+template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, int heads, F f)
 {
     constexpr int most = 16 / (int)sizeof(T);
     int e = most;
-    while (e > 1 && ((rot_dim / 2) % e || (head_dim - rot_dim) % e)) e /= 2;
-    const int units = rot_dim / 2 / e + (head_dim - rot_dim + 2 * e - 1) / (2 * e);
+    const auto units_of = [&](int e) { return rot_dim / 2 / e + (head_dim - rot_dim + 2 * e - 1) / (2 * e); };
+    while (e > 1 && ((rot_dim / 2) % e || (head_dim - rot_dim) % e || heads * units_of(e) <= 32)) e /= 2;
+    const int units = units_of(e);
     const auto pick = [&](auto E) {
         if (units <= 1) return f(E, Is<1>(), Is<1>());
         if (units <= 2) return f(E, Is<1>(), Is<2>());
@@ -337,7 +339,7 @@ hipError_t launch(const void *q, const void *k, const float *wq, const float *wk
     const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads);
     const HeadArgs h = {{{q, gq, oq, wq, s.ld_q, ld_gq, ld_oq, s.q_heads, g.q_parts}, {k, gk, ok, wk, s.ld_k, ld_gk, ld_ok, s.k_heads, g.k_parts}}, pos, freq, part,
                         (int)s.rows, s.head_dim, s.rot_dim, s.interleaved, s.eps};
-    return by_size<T>(s.head_dim, s.rot_dim, [&](auto E, auto NU, auto LPH) {
+    return by_size<T>(s.head_dim, s.rot_dim, s.q_heads > s.k_heads ? s.q_heads : s.k_heads, [&](auto E, auto NU, auto LPH) {
         headnorm_kernel<T, E.value, NU.value, LPH.value, BWD><<<dim3(g.blocks, g.q_parts + g.k_parts), THREADS, 0, st>>>(h);
         return hipGetLastError();
     });
