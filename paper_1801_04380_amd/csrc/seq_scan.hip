@@ -326,16 +326,20 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
     return p;
 }
 
-// Into how many chunks a span is cut when there is workspace for it: a SIMD holds four waves of the forward kernels (a workgroup has
-// one for each) and two of the backward one, and a wave alone leaves more than half of its issue slots empty; twice as many, so that they
-// do not all end together; two tiles each at least.  us with 256, 512, 1024, 2048, 4096 workgroups: forward over 32768 x 1024
-// x 16 501, 320, 264, 256, 267, over 17 ragged sequences, 6000 x 2048 x 16, 209, 144, 127, 123, 137; forward and backward with 256, 512,
-// 1024, 2048 in the backward pass, 8 x 2048 x 2048 x 16 1029, 943, 913, 909, 8193 x 512 x 32 335, 275, 286, 299.
+// Into how many chunks a span is cut when there is workspace for it.
+// Whether at all: a row takes a workgroup 0.145 us (backward 0.33), alone on its compute unit or with another; cut, with the chip full of
+// chunks and the pass for their own states on top, 0.46 ns (1.18 ns) go by a row and workgroup that there would be uncut, and about 14 us (10) for
+// the two launches more.  us whole and cut, 16 states in bf16, 1 x 96 rows of 256 channels: 15.7, 15.3, backward 37.8, 25.9; 8 x 128 x 2048: 21.5, 31.7
+// and 59.8, 68.6; 8 x 512 x 2048: 78, 79 and 189, 177; 8 x 2048 x 2048: 329, 253 and 758, 641; 16 x 2048 x 2048: 389, 473 and 1043, 1252.
+// How far: a SIMD holds four waves of the forward kernels (a workgroup has one for each) and two of the backward one, and a wave alone
+// leaves more than half of its issue slots empty; twice as many, so that they do not all end together; two tiles each at least.  us with 256, 512,
+// 1024, 2048, 4096 workgroups: forward over 32768 x 1024 x 16 501, 320, 264, 256, 267, over 17 ragged sequences, 6000 x 2048 x 16, 209, 144, 127,
+// 123, 137; forward and backward with 256, 512, 1024, 2048 in the backward pass, 8 x 2048 x 2048 x 16 1029, 943, 913, 909, 8193 x 512 x 32 335, 275, 286, 299.
 int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
 {
     const ScanPlan p = scan_plan(s, 1);
     const int64_t have = (int64_t)p.blocks * p.spans, want = bwd ? 1024 : 2048;
-    if (have >= want) return 1;
+    if ((bwd ? 280 - have : 318 - have) * p.span_rows < (bwd ? 8500 : 30000)) return 1;   // the times above, divided by the last rate
     int64_t parts = (want + have - 1) / have;
     const int64_t most = p.tiles_per_span / 2;
     if (parts > most) parts = most;
