@@ -312,10 +312,10 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
     p.CB = 256 / p.NL;
     p.blocks_per_group = div_up(s.channels / s.groups, p.CB);
     p.blocks = p.blocks_per_group * s.groups;
-    // Sequences of equal length are walked each on its own, unless they are no longer than a tile: kept states and sums would be one for
-    // each, where a tile holds several.  4096 x 4 rows of 2048 x 16, us forward and backward, MB of states and workspace: on their own 879, 4054,
+    // Sequences of equal length are walked each on its own, unless they are no longer than a tile and many: kept states and sums would be one for
+    // each, where a tile holds several.  (Few of them are walked side by side that way: 5 x 3 rows of 832 x 16 22 us forward and backward, together 45.)  4096 x 4 rows of 2048 x 16, us forward and backward, MB of states and workspace: on their own 879, 4054,
     // 1152, together 718, 1724, 200; 1024 x 16 rows 278, 1140, 336 and 269, 678, 200.
-    p.spans = s.ragged || s.rows / s.seqs <= TS ? 1 : s.seqs;
+    p.spans = s.ragged || s.rows == 0 || (s.rows / s.seqs <= TS && (int64_t)p.blocks * s.seqs > 1024) ? 1 : s.seqs;
     p.span_rows = (int)(s.rows / p.spans);
     p.tiles_per_span = div_up(p.span_rows, TS);
     if (parts < 1) parts = 1;

@@ -218,6 +218,7 @@ def test_sizes_beyond_the_grids():
 
 
 def test_short_sequences_of_equal_length_share_tiles():
-    together = sn.scan_shape(64 * 4, 64, 16, seqs=64)
-    assert sn.sn_scan_states_bytes(together) == 64 * 4 // 16 * 64 * 16 * 4
+    together = sn.scan_shape(2048 * 4, 64, 16, seqs=2048)
+    assert sn.sn_scan_states_bytes(together) == 2048 * 4 // 16 * 64 * 16 * 4
+    assert sn.sn_scan_states_bytes(sn.scan_shape(64 * 4, 64, 16, seqs=64)) == 64 * 64 * 16 * 4      # few: each on its own
     assert sn.sn_scan_states_bytes(sn.scan_shape(64 * 17, 64, 16, seqs=64)) == 64 * 2 * 64 * 16 * 4
