@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     const float *from = state + ((int64_t)slot * a.channels + c) * a.N, *A = a.A + (int64_t)c * a.N;
     float *to = state_out + ((int64_t)slot * a.channels + c) * a.N;
     const T *B = (const T *)((const char *)a.B + t * a.ld_b) + group * a.N, *C = (const T *)((const char *)a.C + t * a.ld_c) + group * a.N;
-    float h[4], A4[4];
+    float h[4], A2[4];   // A * log2(e) as in the kernels above: delta = 0 leaves a state as it is there and here
     Pack<T, 4> b, cc;
     if (WHOLE) {
         const int n = n0 < a.N ? n0 : 0;
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             h[i] = h4.e[i];
-            A4[i] = a4.e[i];
+            A2[i] = scan_rate(a4.e[i]);
         }
         b.load(B + n);
         cc.load(C + n);
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
         for (int i = 0; i < 4; ++i) {
             const int n = min(n0 + i, a.N - 1);
             h[i] = from[n];
-            A4[i] = A[n];
+            A2[i] = scan_rate(A[n]);
             b.e[i] = B[n];
             cc.e[i] = C[n];
         }
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        h[i] = fmaf(exp_fast(delta * A4[i]), h[i], delta * u * b.get(i));
+        h[i] = fmaf(exp2_fast(delta * A2[i]), h[i], delta * u * b.get(i));
         if (n0 + i < a.N) sum = fmaf(h[i], cc.get(i), sum);
     }
     if (WHOLE) {
