@@ -251,8 +251,8 @@ struct ScanPlan {
     int NL, CB, blocks_per_group, blocks;
     int spans, span_rows, chunk_rows, parts, chunks, tiles_per_span;
 };
-ScanPlan scan_plan(const sn_scan_shape &s, int parts);
-int scan_parts_wanted(const sn_scan_shape &s, bool bwd);
+ScanPlan scan_plan(const sn_scan_shape &s, int parts, bool keeps = true);   // keeps: states of tiles are kept, or made for the gradient
+int scan_parts_wanted(const sn_scan_shape &s, bool bwd, bool keeps = true);
 size_t scan_carry_bytes(const sn_scan_shape &s, const ScanPlan &p);
 ScanArgs scan_args(const sn_scan_shape &s, const ScanPlan &p, const int32_t *off, const void *u, const void *dt, const float *A, const void *B, const void *C,
                    const float *D, const void *z, const float *bias);

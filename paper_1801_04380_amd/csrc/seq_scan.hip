@@ -305,17 +305,34 @@ int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 }  // namespace
 
-ScanPlan scan_plan(const sn_scan_shape &s, int parts)
+// Whether sequences of equal length share tiles and chunks, as ragged ones do, or are walked each on its own (in spans).
+// On its own each has kept states for whole tiles and sums of its own, 4 KB a workgroup each; where tiles and chunks hold several, there are as many as the
+// rows need.  us forward and backward, MB of kept states and workspace, 2048 channels of 16 states in bf16, each on its own and shared:
+//    4096 x 4    879 +  4054, 1152       718 +  1724, 200
+//    4096 x 17  1300 +  4330, 1872      1223 +  3669, 824
+//     512 x 33   241 +   818,  330       274 +   757, 206
+//     129 x 17    45 +   159,   58        76 +   175,  33
+//    1024 x 127 1242 +  4142, 1676      1371 +  4458, 1532
+// Up to a tile's length sharing is faster as soon as there are many; a few are walked side by side instead (5 x 3 rows of 832 x 16: 22 us
+// forward and backward, together 45).  Beyond it, sharing saves no time but memory, and is left out where that is little: up to 8192
+// workgroups own tiles and sums are at most 64 MB more, and from 128 rows on mostly less than an eighth.  A call that keeps no states
+// (keeps false) has nothing to save there.
+static bool shares_tiles(const sn_scan_shape &s, int blocks, bool keeps)
+{
+    if (s.ragged || s.rows == 0) return true;
+    const int64_t len = s.rows / s.seqs, alone = (int64_t)blocks * s.seqs, tiles = (len + TS - 1) / TS;
+    if (len <= TS) return alone > 1024;
+    return keeps && alone > 8192 && 8 * TS * (tiles + 1) > 9 * len;
+}
+
+ScanPlan scan_plan(const sn_scan_shape &s, int parts, bool keeps)
 {
     ScanPlan p;
     p.NL = s.states <= 8 ? 2 : s.states <= 16 ? 4 : s.states <= 32 ? 8 : 16;
     p.CB = 256 / p.NL;
     p.blocks_per_group = div_up(s.channels / s.groups, p.CB);
     p.blocks = p.blocks_per_group * s.groups;
-    // Sequences of equal length are walked each on its own, unless they are no longer than a tile and many: kept states and sums would be one for
-    // each, where a tile holds several.  (Few of them are walked side by side that way: 5 x 3 rows of 832 x 16 22 us forward and backward, together 45.)  4096 x 4 rows of 2048 x 16, us forward and backward, MB of states and workspace: on their own 879, 4054,
-    // 1152, together 718, 1724, 200; 1024 x 16 rows 278, 1140, 336 and 269, 678, 200.
-    p.spans = s.ragged || s.rows == 0 || (s.rows / s.seqs <= TS && (int64_t)p.blocks * s.seqs > 1024) ? 1 : s.seqs;
+    p.spans = shares_tiles(s, p.blocks, keeps) ? 1 : s.seqs;
     p.span_rows = (int)(s.rows / p.spans);
     p.tiles_per_span = div_up(p.span_rows, TS);
     if (parts < 1) parts = 1;
@@ -335,9 +352,9 @@ ScanPlan scan_plan(const sn_scan_shape &s, int parts)
 // leaves more than half of its issue slots empty; twice as many, so that they do not all end together; two tiles each at least.  us with 256, 512,
 // 1024, 2048, 4096 workgroups: forward over 32768 x 1024 x 16 501, 320, 264, 256, 267, over 17 ragged sequences, 6000 x 2048 x 16, 209, 144, 127,
 // 123, 137; forward and backward with 256, 512, 1024, 2048 in the backward pass, 8 x 2048 x 2048 x 16 1029, 943, 913, 909, 8193 x 512 x 32 335, 275, 286, 299.
-int scan_parts_wanted(const sn_scan_shape &s, bool bwd)
+int scan_parts_wanted(const sn_scan_shape &s, bool bwd, bool keeps)
 {
-    const ScanPlan p = scan_plan(s, 1);
+    const ScanPlan p = scan_plan(s, 1, keeps);
     const int64_t have = (int64_t)p.blocks * p.spans, want = bwd ? 1024 : 2048;
     if ((bwd ? 280 - have : 318 - have) * p.span_rows < (bwd ? 8500 : 30000)) return 1;   // the times above, divided by the last rate
     int64_t parts = (want + have - 1) / have;
@@ -414,8 +431,9 @@ hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan
 hipError_t launch_scan_fwd(const void *u, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z, const float *bias, void *y,
                            const sn_scan_shape &s, const int32_t *off, const float *h0, float *hT, float *states, void *ws, size_t ws_bytes, hipStream_t st)
 {
-    ScanPlan p = scan_plan(s, scan_parts_wanted(s, false));
-    while (p.parts > 1 && scan_carry_bytes(s, p) > ws_bytes) p = scan_plan(s, p.parts - 1);
+    const bool keeps = states != nullptr;
+    ScanPlan p = scan_plan(s, scan_parts_wanted(s, false, keeps), keeps);
+    while (p.parts > 1 && scan_carry_bytes(s, p) > ws_bytes) p = scan_plan(s, p.parts - 1, keeps);
     ScanArgs a = scan_args(s, p, off, u, dt, A, B, C, D, z, bias);
     a.y = y; a.h0 = h0; a.hT = hT; a.states = states;
     const int wide = scan_wide(s, p);
