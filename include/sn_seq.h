@@ -69,8 +69,8 @@ sn_status sn_causal_conv1d_step(const void *x, const void *w, const float *bias,
  *   r = 1 / sqrt(mean(x^2) + eps),  n = x * r * weight,
  *   y: (n1, n2) -> (n1 cos a - n2 sin a, n2 cos a + n1 sin a),  a = positions[t] * inv_freq[i]
  * for the pairs i < rot_dim / 2, which are channels (i, i + rot_dim/2) of the head, or (2i, 2i+1) where interleaved; channels
- * from rot_dim on stay n.  The angle is formed in 64 bits: it is as good at position 2^31 as at 1.  positions: int32 [rows], any sign,
- * or NULL for 0, 1, 2 ...; inv_freq: fp32 [rot_dim / 2] (NULL iff rot_dim = 0); wq, wk: fp32 [head_dim], or NULL for ones.
+ * from rot_dim on stay n.  An angle's fraction of a turn is formed in twice 64 bits: it is as good at position 2^31 as at 1.
+ * positions: int32 [rows], any sign, or NULL for 0, 1, 2 ...; inv_freq: fp32 [rot_dim / 2] (NULL iff rot_dim = 0); wq, wk: fp32 [head_dim], or NULL for ones.
  * k may be absent (k_heads = 0, its pointers NULL).  yq may be q and yk k with the same row stride; so may dq be dyq and dk dyk. */
 #define SN_HEADNORM_MAX_DIM 512
 

@@ -105,12 +105,21 @@ template <int E> struct Place {
     __device__ int at_b(int i) const { return pairs ? pa + 2 * i + 1 : pb + i; }
 };
 
-// cos and sin of position * freq: the product and its remainder by whole turns in 64 bits
+// cos and sin of position * freq.  The product of the 31 and 24 bits, and that by 1 / (2 pi), are carried in two doubles each: the fraction of a turn
+// is good to 2^-50 for angles up to 2^50, at far positions and high frequencies alike.  It is rounded to 24 bits because that is what sine and cosine
+// take in 32 bits, and what the rounding took, below 2^-25 of a turn, is put back to first order: sin(a + d) = sin a + d cos a.
 __device__ inline void turn_of(int position, float freq, float &c, float &s)
 {
-    const double turns = (double)position * (double)freq * 0.15915494309189533577;
-    const float part = (float)(turns - rint(turns));
-    sincospif(2.f * part, &s, &c);
+#pragma clang fp contract(off)   // each product by itself: what it lost is added by the line after it
+    constexpr double turn = 0.15915494309189535, turn_lo = -9.839338337591243e-18;   // 1 / (2 pi)
+    const double p = (double)position, f = (double)freq, angle = p * f, turns = angle * turn;
+    const double lost = fma(angle, turn, -turns) + (angle * turn_lo + fma(p, f, -angle) * turn);
+    const double part = (turns - rint(turns)) + lost, left = part - rint(part);
+    const float near = (float)left, rest = (float)(left - (double)near) * 6.28318530717958647692f;
+    float c0, s0;
+    sincospif(2.f * near, &s0, &c0);
+    c = fmaf(-s0, rest, c0);
+    s = fmaf(c0, rest, s0);
 }
 
 // The sum over the LPH lanes of a head, in each of them.  Within 16 lanes by the cross-lane operands of the addition: neighbours, pairs,
