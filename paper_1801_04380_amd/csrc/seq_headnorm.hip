@@ -136,6 +136,14 @@ template <int LPH> __device__ inline float head_sum(float v)
     return v;
 }
 
+// 1 / sqrt(v) within one unit of the last place.  The instruction takes numbers below 2^-126 for zero: they are scaled, by a power of four.
+__device__ inline float inv_root(float v)
+{
+    const bool small = v < 0x1p-126f;
+    const float r = __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v);
+    return small ? r * 0x1p32f : r;
+}
+
 template <typename T, int E, int NU, int LPH, bool BWD>
 __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
 {
@@ -208,7 +216,7 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
             }
             const bool more = hb + HPW < h1;
             fetch(more ? row : row + stride, more ? head + HPW : h0 + group);
-            const float r = __builtin_amdgcn_rsqf(fmaf(head_sum<LPH>(sum), inv_dim, h.eps));
+            const float r = inv_root(fmaf(head_sum<LPH>(sum), inv_dim, h.eps));
             if (!BWD) {
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
