@@ -211,9 +211,10 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a, int reverse)
         for (int k = 0; k < AT; ++k) {
             *to = v;
             to += step;
-            // a state of 0 stays 0, also through a factor past the range (growing states before the first input)
-            const float in = keep_if(through[k], v), factor = keep_if(in != 0.f, exp2_fast(A2 * sum[k]));
-            v = fmaf(factor, in, local[k]);
+            // The factor in two halves: between two states in range it may be beyond it (from 2^-126 to 2^127), its root is not.  A state of 0
+            // stays 0, also through a root past the range (growing states before the first input).
+            const float in = keep_if(through[k], v), root = keep_if(in != 0.f, exp2_fast(0.5f * (A2 * sum[k])));
+            v = fmaf(root, root * in, local[k]);
         }
     };
     int k = 0;   // the last chunk hands on to nothing: it has no values
