@@ -106,6 +106,19 @@ __device__ inline float softplus(float x)
     return x > 20.f ? x : r;
 }
 
+// A sum of any number of values: off by one rounding of it, and by n * 2^-47 of the n values' magnitudes.  What an addition loses is a number of 32 bits again and
+// is summed by itself (Knuth, The Art of Computer Programming, 4.2.2, theorem B).  A sum past the range stays infinite.
+struct LongSum {
+    float s = 0.f, lost = 0.f;
+    __device__ void add(float v)
+    {
+        const float t = s + v, of_v = t - s;
+        lost += (s - (t - of_v)) + (v - of_v);
+        s = t;
+    }
+    __device__ float total() const { return lost == lost ? s + lost : s; }
+};
+
 // a slot index of a step call: row -> slot, or -1 for a row to skip
 __device__ inline int step_slot(const int32_t *slots, int row, int num_slots)
 {

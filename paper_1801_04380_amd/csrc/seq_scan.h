@@ -13,6 +13,10 @@
 namespace sn {
 
 constexpr int TS = 16;   // rows between two kept states; of a tile in the backward pass
+// Rows (and up to a tile more) after which the gradients' sums over rows start from zero again, and what they were is added to what is in the workspace without loss.  A
+// running sum of n terms is off by up to n * 2^-24 of them (over 2^20 equal rows dA was off by 0.6 %); like this by 2^-16 at most, and by about 2^-21 where
+// the roundings are as often up as down.
+constexpr int SUM_ROWS = 256;
 
 template <int NL> struct ScanGeo {
     static constexpr int CW = 64 / NL, CB = 4 * CW, NP = 4 * NL;
@@ -34,6 +38,7 @@ struct ScanArgs {
     int *through;                                             // [chunk]: no sequence ends and begins in it
     int NP;                                                   // the states of the library's own arrays: padded to four for each lane
     float *part_a, *part_d, *part_bias, *part_bc;             // sums of chunks; of channel blocks [block][row][2][NP]
+    int64_t lost;   // what the sums of chunks have lost so far is so many elements behind each of them; 0: chunks of SUM_ROWS at most, whose sums are added once
     int gate;   // z is there; if not, z is u: loaded and left out
 };
 

@@ -323,7 +323,8 @@ static bool shares_tiles(const sn_scan_shape &s, int blocks, bool keeps)
     if (s.ragged || s.rows == 0) return true;
     const int64_t len = s.rows / s.seqs, alone = (int64_t)blocks * s.seqs, tiles = (len + TS - 1) / TS;
     if (len <= TS) return alone > 1024;
-    return keeps && alone > 8192 && 8 * TS * (tiles + 1) > 9 * len;
+    const int64_t own = tiles + (len > SUM_ROWS ? 2 : 1);   // of 4 KB: tiles, sums, what the sums have lost
+    return keeps && alone > 8192 && 8 * TS * own > 9 * len;
 }
 
 ScanPlan scan_plan(const sn_scan_shape &s, int parts, bool keeps)

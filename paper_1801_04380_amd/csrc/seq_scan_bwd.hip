@@ -156,6 +156,53 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
     float g[4] = {0.f, 0.f, 0.f, 0.f};
     if (part < a.parts - 1) lane.load_own(a.carry, chunk, a, g);
 
+    // The sums since the last time are added to what is in the workspace; those of dD and the bias's gradient over the 16 threads that stage a channel.
+    bool begun = false;
+    const auto add_sums = [&](bool last) {
+        int at = chunk, tid = threadIdx.x;
+        asm volatile("" : "+s"(at), "+v"(tid));   // addresses are formed here, not in front of the loop, through which they would take a dozen registers
+        LongSum sum[4];
+        float s[4] = {0.f, 0.f, 0.f, 0.f}, lost[4] = {0.f, 0.f, 0.f, 0.f};
+        if (begun) {
+            lane.load_own(a.part_a, at, a, s);
+            lane.load_own(a.part_a + a.lost, at, a, lost);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sum[i].s = s[i];
+            sum[i].lost = lost[i];
+            sum[i].add(dA[i]);
+            s[i] = last ? sum[i].total() : sum[i].s;
+            lost[i] = sum[i].lost;
+            dA[i] = 0.f;
+        }
+        lane.store_own(a.part_a, at, a, s);
+        if (!last) lane.store_own(a.part_a + a.lost, at, a, lost);
+        __syncthreads();
+        for (int k = tid; k < 2 * CB; k += THREADS) {
+            const int c = k % CB;
+            float rows = 0.f;
+#pragma unroll
+            for (int r = 0; r < TS; ++r) rows += k < CB ? s_dD[r][c] : s_dbias[r][c];
+            if (c >= nch) continue;
+            float *to = (k < CB ? a.part_d : a.part_bias) + (int64_t)at * a.channels + c0 + c;
+            LongSum all;
+            if (begun) {
+                all.s = to[0];
+                all.lost = to[a.lost];
+            }
+            all.add(rows);
+            to[0] = last ? all.total() : all.s;
+            if (!last) to[a.lost] = all.lost;
+        }
+        begun = true;
+        if (last) return;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VE; ++i) s_dD[row][co + i] = s_dbias[row][co + i] = 0.f;
+    };
+    int sum_to = a.lost ? r1 - SUM_ROWS : -1;   // the row that the sums go on to
+
     if (r0 < r1) {
         SeqAt at = seq_find(a.rows, r1 - 1);
         Piece next = piece_before<TS>(a.rows, at, r1, r0);
@@ -206,165 +253,163 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
             if (next.any) fetch();
         }
         __syncthreads();
-        while (now.any) {
-            if (now.end) {
-                if (a.dhT) lane.load(a.dhT, now.seq, a, g);
-                else g[0] = g[1] = g[2] = g[3] = 0.f;
-            }
-
-            constexpr int TB = CW < 8 ? 1 : CW / 8;       // rows whose 8 values share the exchanges over channels
-            constexpr int GR = NL > TB ? NL : TB;         // rows that are worked on or left out together
-            constexpr int HR = GR > 8 ? GR : 8;           // rows whose states are in registers at a time
-            const auto read = [&](int t) {
-                RowIn r;
-                r.d = s_delta[t][lane.c];
-                r.x = s_x[t][lane.c];
-                r.g = s_g[t][lane.c];
-                *reinterpret_cast<float4 *>(r.b) = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
-                *reinterpret_cast<float4 *>(r.c) = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
-                return r;
-            };
-            const auto outside = [&](int tb, int n) { return now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1; };
-            {
-                // the state in front of the second half
-                float mid[4] = {first[0], first[1], first[2], first[3]};
-                if (HR < TS && !outside(0, HR)) {
-                    RowIn r, ahead = read(0);
-#pragma unroll
-                    for (int t = 0; t < HR; ++t) {
-                        r = ahead;
-                        ahead = read(t + 1 < HR ? t + 1 : t);
-                        ROW_AHEAD();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(r.d * lane.A2[i]), mid[i], r.x * r.b[i]);
-                    }
+        int done;
+        while (now.any) {   // a stretch of SUM_ROWS a turn: what adds up its sums would take registers of the loop over its pieces, if it stood in there
+            do {
+                if (now.end) {
+                    if (a.dhT) lane.load(a.dhT, now.seq, a, g);
+                    else g[0] = g[1] = g[2] = g[3] = 0.f;
                 }
-#pragma unroll 1
-                for (int half = TS - HR; half >= 0; half -= HR) {
-                    float hs[HR + 1][4], decay[HR][4];   // hs[k]: the state in front of the half's row k
+
+                constexpr int TB = CW < 8 ? 1 : CW / 8;       // rows whose 8 values share the exchanges over channels
+                constexpr int GR = NL > TB ? NL : TB;         // rows that are worked on or left out together
+                constexpr int HR = GR > 8 ? GR : 8;           // rows whose states are in registers at a time
+                const auto read = [&](int t) {
+                    RowIn r;
+                    r.d = s_delta[t][lane.c];
+                    r.x = s_x[t][lane.c];
+                    r.g = s_g[t][lane.c];
+                    *reinterpret_cast<float4 *>(r.b) = *reinterpret_cast<const float4 *>(&s_B[t * NP + lane.n0]);
+                    *reinterpret_cast<float4 *>(r.c) = *reinterpret_cast<const float4 *>(&s_C[t * NP + lane.n0]);
+                    return r;
+                };
+                const auto outside = [&](int tb, int n) { return now.t0 + tb + n <= now.p0 || now.t0 + tb >= now.p1; };
+                {
+                    // the state in front of the second half
+                    float mid[4] = {first[0], first[1], first[2], first[3]};
+                    if (HR < TS && !outside(0, HR)) {
+                        RowIn r, ahead = read(0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) hs[0][i] = half ? mid[i] : first[i];
-                    // the states, forwards; rows that are not the piece's leave them as they are
-#pragma unroll
-                    for (int kb = 0; kb < HR; kb += GR) {
-                        float acc[NL];
-                        RowIn r, ahead = read(half + kb);
-#pragma unroll
-                        for (int k = kb; k < kb + GR; ++k) {
-                            const int t = half + k;
+                        for (int t = 0; t < HR; ++t) {
                             r = ahead;
-                            ahead = read(k + 1 < HR ? t + 1 : t);
+                            ahead = read(t + 1 < HR ? t + 1 : t);
                             ROW_AHEAD();
-                            float sum = 0.f;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                decay[k][i] = exp2_fast(r.d * lane.A2[i]);
-                                hs[k + 1][i] = fmaf(decay[k][i], hs[k][i], r.x * r.b[i]);
-                                sum = fmaf(hs[k + 1][i], r.c[i], sum);
-                            }
-                            acc[t % NL] = sum;
-                            if (t % NL == NL - 1) s_y[t / NL * NL + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
+                            for (int i = 0; i < 4; ++i) mid[i] = fmaf(exp2_fast(r.d * lane.A2[i]), mid[i], r.x * r.b[i]);
                         }
                     }
-                    // and the gradients, backwards; what the rows' operands took in registers is read again
-                    asm volatile("" ::: "memory");
+#pragma unroll 1
+                    for (int half = TS - HR; half >= 0; half -= HR) {
+                        float hs[HR + 1][4], decay[HR][4];   // hs[k]: the state in front of the half's row k
 #pragma unroll
-                    for (int kb = HR - GR; kb >= 0; kb -= GR) {
-                        if (outside(half + kb, GR)) continue;
-                        float gb[NL], qa[NL], bc[8 * TB];
-                        RowIn r, ahead = read(half + kb + GR - 1);
+                        for (int i = 0; i < 4; ++i) hs[0][i] = half ? mid[i] : first[i];
+                        // the states, forwards; rows that are not the piece's leave them as they are
 #pragma unroll
-                        for (int k = kb + GR - 1; k >= kb; --k) {
-                            const int t = half + k;
-                            r = ahead;
-                            ahead = read(k ? t - 1 : t);
-                            ROW_AHEAD();
-                            float sum_b = 0.f, sum_a = 0.f;
+                        for (int kb = 0; kb < HR; kb += GR) {
+                            float acc[NL];
+                            RowIn r, ahead = read(half + kb);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float gi = fmaf(r.g, r.c[i], g[i]);
-                                bc[t % TB * 8 + i] = gi * r.x;
-                                bc[t % TB * 8 + 4 + i] = r.g * hs[k + 1][i];
-                                sum_b = fmaf(gi, r.b[i], sum_b);
-                                g[i] = decay[k][i] * gi;
-                                const float q = g[i] * hs[k][i];
-                                sum_a = fmaf(q, lane.A2[i], sum_a);
-                                dA[i] = fmaf(q, r.d, dA[i]);
+                            for (int k = kb; k < kb + GR; ++k) {
+                                const int t = half + k;
+                                r = ahead;
+                                ahead = read(k + 1 < HR ? t + 1 : t);
+                                ROW_AHEAD();
+                                float sum = 0.f;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    decay[k][i] = exp2_fast(r.d * lane.A2[i]);
+                                    hs[k + 1][i] = fmaf(decay[k][i], hs[k][i], r.x * r.b[i]);
+                                    sum = fmaf(hs[k + 1][i], r.c[i], sum);
+                                }
+                                acc[t % NL] = sum;
+                                if (t % NL == NL - 1) s_y[t / NL * NL + nl][lane.c] = scatter_sum<NL / 2, 1>(acc);
                             }
-                            gb[t % NL] = sum_b;
-                            qa[t % NL] = sum_a;
-                            if (t % NL == 0) {   // rows t .. t + NL - 1 are done
-                                s_x[t + nl][lane.c] = scatter_sum<NL / 2, 1>(gb);   // over what the rows were staged with
-                                s_qa[t + nl][lane.c] = scatter_sum<NL / 2, 1>(qa);
-                            }
-                            if (t % TB == 0) {
-                                const int k8 = scan_lane() / NL;   // which of the rows' values this lane gets
-                                if constexpr (CW >= 8) {
-                                    s_bc[wave][t + k8 / 8][(k8 / 4 & 1) * NP + lane.n0 + k8 % 4] = scatter_sum<32, NL>(bc);
-                                } else {
-                                    float lo[4] = {bc[0], bc[1], bc[2], bc[3]}, hi[4] = {bc[4], bc[5], bc[6], bc[7]};
-                                    s_bc[wave][t][lane.n0 + k8] = scatter_sum<32, NL>(lo);
-                                    s_bc[wave][t][NP + lane.n0 + k8] = scatter_sum<32, NL>(hi);
+                        }
+                        // and the gradients, backwards; what the rows' operands took in registers is read again
+                        asm volatile("" ::: "memory");
+#pragma unroll
+                        for (int kb = HR - GR; kb >= 0; kb -= GR) {
+                            if (outside(half + kb, GR)) continue;
+                            float gb[NL], qa[NL], bc[8 * TB];
+                            RowIn r, ahead = read(half + kb + GR - 1);
+#pragma unroll
+                            for (int k = kb + GR - 1; k >= kb; --k) {
+                                const int t = half + k;
+                                r = ahead;
+                                ahead = read(k ? t - 1 : t);
+                                ROW_AHEAD();
+                                float sum_b = 0.f, sum_a = 0.f;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const float gi = fmaf(r.g, r.c[i], g[i]);
+                                    bc[t % TB * 8 + i] = gi * r.x;
+                                    bc[t % TB * 8 + 4 + i] = r.g * hs[k + 1][i];
+                                    sum_b = fmaf(gi, r.b[i], sum_b);
+                                    g[i] = decay[k][i] * gi;
+                                    const float q = g[i] * hs[k][i];
+                                    sum_a = fmaf(q, lane.A2[i], sum_a);
+                                    dA[i] = fmaf(q, r.d, dA[i]);
+                                }
+                                gb[t % NL] = sum_b;
+                                qa[t % NL] = sum_a;
+                                if (t % NL == 0) {   // rows t .. t + NL - 1 are done
+                                    s_x[t + nl][lane.c] = scatter_sum<NL / 2, 1>(gb);   // over what the rows were staged with
+                                    s_qa[t + nl][lane.c] = scatter_sum<NL / 2, 1>(qa);
+                                }
+                                if (t % TB == 0) {
+                                    const int k8 = scan_lane() / NL;   // which of the rows' values this lane gets
+                                    if constexpr (CW >= 8) {
+                                        s_bc[wave][t + k8 / 8][(k8 / 4 & 1) * NP + lane.n0 + k8 % 4] = scatter_sum<32, NL>(bc);
+                                    } else {
+                                        float lo[4] = {bc[0], bc[1], bc[2], bc[3]}, hi[4] = {bc[4], bc[5], bc[6], bc[7]};
+                                        s_bc[wave][t][lane.n0 + k8] = scatter_sum<32, NL>(lo);
+                                        s_bc[wave][t][NP + lane.n0 + k8] = scatter_sum<32, NL>(hi);
+                                    }
                                 }
                             }
                         }
                     }
                 }
-            }
-            if (a.dh0 && now.start) lane.store(a.dh0, now.seq, a, g);
-            __syncthreads();
-            const bool in = now.holds(now.t0 + row);
-            Staged<T, NL, WIDE> du, ddt, dz;
+                if (a.dh0 && now.start) lane.store(a.dh0, now.seq, a, g);
+                __syncthreads();
+                const bool in = now.holds(now.t0 + row);
+                Staged<T, NL, WIDE> du, ddt, dz;
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                const float vb = s_x[row][co + i], va = s_qa[row][co + i] * 0.69314718055994530942f /* A is A2 * ln 2 */, gy = s_g[row][co + i];
-                const float dd = fmaf(uu[i], vb, va) * slope[i];
-                du.set(i, fmaf(gy, s_skip[co + i], s_delta[row][co + i] * vb));
-                ddt.set(i, dd);
-                dz.set(i, zslope[i] * fmaf(s_skip[co + i], uu[i], s_y[row][co + i]));
-                const bool here = in && i < nco;
-                s_dbias[row][co + i] += keep_if(here, dd);
-                s_dD[row][co + i] = fmaf(gy, uu[i], s_dD[row][co + i]);   // both are zero elsewhere
-            }
-            constexpr int PER = (TS * 2 * NP / 4 + THREADS - 1) / THREADS;
-            float4 bc[PER];
+                for (int i = 0; i < VE; ++i) {
+                    const float vb = s_x[row][co + i], va = s_qa[row][co + i] * 0.69314718055994530942f /* A is A2 * ln 2 */, gy = s_g[row][co + i];
+                    const float dd = fmaf(uu[i], vb, va) * slope[i];
+                    du.set(i, fmaf(gy, s_skip[co + i], s_delta[row][co + i] * vb));
+                    ddt.set(i, dd);
+                    dz.set(i, zslope[i] * fmaf(s_skip[co + i], uu[i], s_y[row][co + i]));
+                    const bool here = in && i < nco;
+                    s_dbias[row][co + i] += keep_if(here, dd);
+                    s_dD[row][co + i] = fmaf(gy, uu[i], s_dD[row][co + i]);   // both are zero elsewhere
+                }
+                constexpr int PER = (TS * 2 * NP / 4 + THREADS - 1) / THREADS;
+                float4 bc[PER];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int k = i * THREADS + threadIdx.x, r = k * 4 / (2 * NP) % TS, n = k * 4 % (2 * NP);
-                const auto at = [&](int w) { return *reinterpret_cast<const float4 *>(&s_bc[w][r][n]); };
-                const float4 p = at(0), q = at(1), v = at(2), w = at(3);
-                bc[i] = make_float4(p.x + q.x + v.x + w.x, p.y + q.y + v.y + w.y, p.z + q.z + v.z + w.z, p.w + q.w + v.w + w.w);
-            }
-            // The next rows are staged before anything is stored: whoever waits for the loads waits for what was stored since as well.
-            if (next.any) stage(next);
-            if (in) {
-                du.store(pdu + (int64_t)now.t0 * a.ld_du, a.ld_du, row, co, nch);
-                ddt.store(pddt + (int64_t)now.t0 * a.ld_ddt, a.ld_ddt, row, co, nch);
-                if (a.gate) dz.store(pdz + (int64_t)now.t0 * a.ld_dz, a.ld_dz, row, co, nch);
-            }
+                for (int i = 0; i < PER; ++i) {
+                    const int k = i * THREADS + threadIdx.x, r = k * 4 / (2 * NP) % TS, n = k * 4 % (2 * NP);
+                    const auto at = [&](int w) { return *reinterpret_cast<const float4 *>(&s_bc[w][r][n]); };
+                    const float4 p = at(0), q = at(1), v = at(2), w = at(3);
+                    bc[i] = make_float4(p.x + q.x + v.x + w.x, p.y + q.y + v.y + w.y, p.z + q.z + v.z + w.z, p.w + q.w + v.w + w.w);
+                }
+                // The next rows are staged before anything is stored: whoever waits for the loads waits for what was stored since as well.
+                if (next.any) stage(next);
+                if (in) {
+                    du.store(pdu + (int64_t)now.t0 * a.ld_du, a.ld_du, row, co, nch);
+                    ddt.store(pddt + (int64_t)now.t0 * a.ld_ddt, a.ld_ddt, row, co, nch);
+                    if (a.gate) dz.store(pdz + (int64_t)now.t0 * a.ld_dz, a.ld_dz, row, co, nch);
+                }
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t k = i * THREADS + threadIdx.x, r = k * 4 / (2 * NP);
-                if (r < TS && now.holds(now.t0 + r)) *reinterpret_cast<float4 *>(part_bc + (int64_t)now.t0 * (2 * NP) + k * 4) = bc[i];
-            }
-            now = next;
-            if (now.any) {
-                next = piece_before<TS>(a.rows, at, now.p0, r0);
-                if (next.any) fetch();
-            }
-            __syncthreads();
+                for (int i = 0; i < PER; ++i) {
+                    const uint32_t k = i * THREADS + threadIdx.x, r = k * 4 / (2 * NP);
+                    if (r < TS && now.holds(now.t0 + r)) *reinterpret_cast<float4 *>(part_bc + (int64_t)now.t0 * (2 * NP) + k * 4) = bc[i];
+                }
+                done = now.p0;
+                now = next;
+                if (now.any) {
+                    next = piece_before<TS>(a.rows, at, now.p0, r0);
+                    if (next.any) fetch();
+                }
+                __syncthreads();
+            } while (now.any && done > sum_to);
+            if (!now.any) break;
+            sum_to = done - SUM_ROWS;
+            add_sums(false);
         }
     }
-    lane.store_own(a.part_a, chunk, a, dA);
-    // dD and the bias's gradient: over the 16 threads that stage a channel
-    __syncthreads();
-    for (int k = threadIdx.x; k < 2 * CB; k += THREADS) {
-        const int c = k % CB;
-        float sum = 0.f;
-#pragma unroll
-        for (int r = 0; r < TS; ++r) sum += k < CB ? s_dD[r][c] : s_dbias[r][c];
-        if (c < nch) (k < CB ? a.part_d : a.part_bias)[(int64_t)chunk * a.channels + c0 + c] = sum;
-    }
+    add_sums(true);
     if (a.dh0 && chunk == 0 && (a.rows.off || a.rows.rows == 0))
         each_empty(a.rows, [&](int s) {   // the gradients of their states pass through
             float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -406,17 +451,16 @@ __global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int grou
     if (i < each) { from = a.part_a + i / a.N * (a.NP - a.N); to = dA; at = i; stride = (int64_t)a.channels * a.NP; }
     else if (i < each + a.channels) { from = a.part_d; to = dD; at = i - each; }
     else if (i < each + 2 * (int64_t)a.channels) { from = a.part_bias; to = dbias; at = i - each - a.channels; }
-    float sum = 0.f;
+    LongSum sum, all;
     if (to)
 #pragma unroll 8
-        for (int c = lane; c < chunks; c += 16) sum += from[c * stride + at];
-    lds[lane][threadIdx.x % 16] = sum;
+        for (int c = lane; c < chunks; c += 16) sum.add(from[c * stride + at]);
+    lds[lane][threadIdx.x % 16] = sum.total();
     __syncthreads();
     if (lane || !to) return;
-    sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < 16; ++c) sum += lds[c][threadIdx.x];
-    to[at] = sum;
+    for (int c = 0; c < 16; ++c) all.add(lds[c][threadIdx.x]);
+    to[at] = all.total();
 }
 
 template <typename T, int NL, int WIDE> hipError_t bwd_in_chunks(const ScanArgs &a, const ScanPlan &p, hipStream_t st)
@@ -433,8 +477,8 @@ template <typename T, int NL, int WIDE> hipError_t bwd_in_chunks(const ScanArgs 
 }
 
 struct BwdBytes {
-    size_t carry, a, d, bc;
-    size_t all() const { return carry + a + 2 * d + bc; }
+    size_t carry, a, d, lost, bc;
+    size_t all() const { return carry + a + 2 * d + lost + bc; }
 };
 
 BwdBytes bytes_of(const sn_scan_shape &s, const ScanPlan &p)
@@ -443,6 +487,7 @@ BwdBytes bytes_of(const sn_scan_shape &s, const ScanPlan &p)
     b.carry = scan_carry_bytes(s, p);
     b.a = align_up((size_t)p.chunks * s.channels * 4 * p.NL * 4, 256);
     b.d = align_up((size_t)p.chunks * s.channels * 4, 256);
+    b.lost = p.chunk_rows > SUM_ROWS ? b.a + 2 * b.d : 0;
     b.bc = align_up((size_t)p.blocks * s.rows * 8 * p.NL * 4, 256);
     return b;
 }
@@ -474,6 +519,7 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
     a.part_a = (float *)at; at += b.a;
     a.part_d = (float *)at; at += b.d;
     a.part_bias = (float *)at; at += b.d;
+    a.lost = b.lost / 4; at += b.lost;
     a.part_bc = (float *)at;
     hipError_t e = hipSuccess;
     if (!states && s.rows) e = launch_scan_states(a, s, p, wide, st);

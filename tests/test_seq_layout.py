@@ -21,7 +21,7 @@ def test_many_sequences_of_few_tiles_take_what_ragged_ones_take(L, channels, sta
 def test_memory_has_no_step(S, states):
     """One token more a sequence than a whole number of tiles: within 72 MB, or an eighth, of what the same rows take as ragged sequences, kept
     states and the least workspace together."""
-    for L in list(range(1, 60)) + [127, 128, 129, 145, 1025]:
+    for L in list(range(1, 60)) + [127, 128, 129, 145, 255, 256, 257, 273, 1025]:
         kept, _, (least, _) = bytes_of(L, S, 1536, states, False)
         rkept, _, (rleast, _) = bytes_of(L, S, 1536, states, True)
         assert kept + least <= (rkept + rleast) * 9 / 8 + (72 << 20), L
