@@ -148,11 +148,12 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
                                                              const T *__restrict__ dstate_out)
 {
     constexpr int R = W <= 5 ? 8 : 16, H = W - 1;
-    if ((blockIdx.x * THREADS + threadIdx.x) * V >= channels) return;
-    const int c = min((int)(blockIdx.x * THREADS + threadIdx.x) * V, channels - V);
+    const unsigned blocks = (channels + V * THREADS - 1) / (V * THREADS), slice = blockIdx.x / blocks, first = (blockIdx.x % blocks * THREADS + threadIdx.x) * V;
+    if (first >= (unsigned)channels) return;
+    const int c = min((int)first, channels - V);
     Taps<T, V, W> taps;
     taps.load(w, bias, c);
-    const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
+    const int r0 = slice * run, r1 = min(r0 + run, rows.rows);
     float dw[V][W] = {}, db[V] = {};
     if (r0 < r1) {
         float in[H + R][V] = {}, dp[H + R][V] = {};   // x and dp of rows b .. b + R + H - 1
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(THREADS) conv1d_bwd_kernel(const T *__restrict
                 }
         }
     }
-    float *to = part + (size_t)blockIdx.y * (W + 1) * channels + c;
+    float *to = part + (size_t)slice * (W + 1) * channels + c;
 #pragma unroll
     for (int j = 0; j <= W; ++j) {
         Pack<float, V> v;
@@ -310,18 +311,17 @@ __global__ void __launch_bounds__(THREADS) conv1d_sum_kernel(const float *__rest
 {
     __shared__ float sums[16][16];
     const int lane = threadIdx.x / 16, c = blockIdx.x * 16 + threadIdx.x % 16, j = blockIdx.y;
-    float sum = 0.f;
+    LongSum sum, all;
     if (c < channels)
 #pragma unroll 8
-        for (int s = lane; s < slices; s += 16) sum += part[((size_t)s * (width + 1) + j) * channels + c];
-    sums[lane][threadIdx.x % 16] = sum;
+        for (int s = lane; s < slices; s += 16) sum.add(part[((size_t)s * (width + 1) + j) * channels + c]);
+    sums[lane][threadIdx.x % 16] = sum.total();
     __syncthreads();
     if (lane || c >= channels) return;
-    sum = 0.f;
 #pragma unroll
-    for (int s = 0; s < 16; ++s) sum += sums[s][threadIdx.x];
-    if (j < width) dw[(size_t)c * width + j] = sum;
-    else if (dbias) dbias[c] = sum;
+    for (int s = 0; s < 16; ++s) all.add(sums[s][threadIdx.x]);
+    if (j < width) dw[(size_t)c * width + j] = all.total();
+    else if (dbias) dbias[c] = all.total();
 }
 
 template <typename T, int V, int W>
@@ -403,7 +403,13 @@ template <typename T> hipError_t fwd(const void *x, const void *w, const float *
 
 constexpr int BWD_V = 4;   // channels of a thread at most: with 8 the windows of x and dp alone would take 176 registers
 
-int bwd_run(int64_t rows, int channels) { return run_of(rows, div_up(channels, BWD_V * THREADS), 64); }   // 64 rows: the turn that fills the windows costs little
+// 64 rows at least, so that the turn that fills the windows costs little, and 256 at most: the sums for dw and dbias are running sums over them, off by up to
+// 2^-24 of the terms for each (over 2^24 equal rows in 512 runs 3e-4); the slices' sums are joined without loss.
+int bwd_run(int64_t rows, int channels)
+{
+    const int run = run_of(rows, div_up(channels, BWD_V * THREADS), 64);
+    return run > 256 ? 256 : run;
+}
 
 template <typename T> hipError_t bwd(const void *x, const void *w, const float *bias, const void *dy, void *dx, float *dw, float *dbias, const sn_conv1d_shape &s,
                                      const int32_t *off, const void *state_in, const void *dstate_out, void *dstate_in, void *scratch, hipStream_t st)
@@ -412,7 +418,7 @@ template <typename T> hipError_t bwd(const void *x, const void *w, const float *
         const int run = bwd_run(s.rows, s.channels), slices = s.rows ? div_up(s.rows, run) : 1;
         const SeqRows rows = rows_of(s, off);
         hipError_t e = by_vector<BWD_V, false>(s.channels, [&](auto V) {
-            conv1d_bwd_kernel<T, V.value, W.value><<<dim3(div_up(s.channels, V.value * THREADS), slices), THREADS, 0, st>>>(
+            conv1d_bwd_kernel<T, V.value, W.value><<<(unsigned)div_up(s.channels, V.value * THREADS) * slices, THREADS, 0, st>>>(
                 (const T *)x, (const T *)w, bias, (const T *)dy, (T *)dx, (float *)scratch, s.channels, s.silu, s.ld_x, s.ld_y, s.ld_dx, rows, run,
                 (const T *)state_in, (const T *)dstate_out);
             return hipGetLastError();

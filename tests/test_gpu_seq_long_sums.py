@@ -43,3 +43,13 @@ def test_scan(ragged, cut, D, N):
         assert off(got, S * want[k]) <= SUM + 96 * 2.0 ** -24, k
     for got, k in ((du, "du"), (dB, "dB"), (dz, "dz")):
         assert off(got[-L:], want[k]) <= 192 * 2.0 ** -24, k
+
+
+def test_conv1d():
+    rows, D, W = 1 << 24, 4, 4
+    x, dy, w = torch.full((rows, D), 0.7, device="cuda"), torch.full((rows, D), 0.3, device="cuda"), torch.ones(D, W, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.full((D, W), SENTINEL, device="cuda"), torch.full((D,), SENTINEL, device="cuda")
+    sn.sn_causal_conv1d_bwd(x, w, None, dy, dx, dw, db, bytes_(sn.sn_causal_conv1d_scratch_bytes(rows, D, W)), silu=False)
+    a, b = float(np.float32(0.7)), float(np.float32(0.3))
+    assert off(db, np.full(D, rows * b)) <= SUM
+    assert off(dw, np.repeat([(rows - W + 1 + np.arange(W)) * a * b], D, 0)) <= SUM + 2.0 ** -24
