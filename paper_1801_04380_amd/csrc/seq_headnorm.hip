@@ -293,32 +293,39 @@ __global__ void __launch_bounds__(1024) headnorm_sum_kernel(const float *__restr
 {
     const int e = threadIdx.x % 16, lane = threadIdx.x / 16, i = blockIdx.x * 16 + e, first = blockIdx.y ? q_parts : 0, count = blockIdx.y ? k_parts : q_parts;
     __shared__ float sums[64][16];
-    float s = 0.f;
+    LongSum s, all;
     if (i < head_dim)
 #pragma unroll 8
-        for (int p = lane; p < count; p += 64) s += part[(size_t)(first + p) * head_dim + i];
-    sums[lane][e] = s;
+        for (int p = lane; p < count; p += 64) s.add(part[(size_t)(first + p) * head_dim + i]);
+    sums[lane][e] = s.total();
     __syncthreads();
     float *to = blockIdx.y ? dwk : dwq;
     if (lane || i >= head_dim || !to) return;
-    s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 64; ++j) s += sums[j][e];
-    to[i] = s;
+    for (int j = 0; j < 64; ++j) all.add(sums[j][e]);
+    to[i] = all.total();
 }
 
-// How many workgroups walk the rows, and into how many parts the lists of heads are cut: waves for the chip where rows are few.
+// How many workgroups walk the rows, and into how many parts the lists of heads are cut: waves for the chip where rows are few.  Backward (sums): as many more as
+// it takes for a lane to add up 256 terms of a weight's gradient at most (a running sum is off by up to 2^-24 of the terms for each: over 2^25 equal rows in 1024
+// workgroups 9e-5); the workgroups' sums are joined without loss.
 struct HeadGrid {
     int blocks, q_parts, k_parts;
 };
-HeadGrid grid_of(int64_t rows, int q_heads, int k_heads)
+HeadGrid grid_of(int64_t rows, int q_heads, int k_heads, bool sums)
 {
+    constexpr int64_t TERMS = 256;
     HeadGrid g;
-    const int64_t blocks = (rows + WAVES - 1) / WAVES;
-    g.blocks = (int)(blocks > 1024 ? 1024 : blocks < 1 ? 1 : blocks);
-    const int parts = 1024 / g.blocks;
-    g.q_parts = parts < q_heads ? parts : q_heads;
-    g.k_parts = parts < k_heads ? parts : k_heads;
+    const int64_t most = (rows + WAVES - 1) / WAVES, heads = q_heads > k_heads ? q_heads : k_heads;
+    int64_t blocks = most > 1024 ? 1024 : most < 1 ? 1 : most, parts = 1024 / blocks;
+    if (sums) {
+        if (heads > parts * TERMS) parts = (heads + TERMS - 1) / TERMS;
+        const int64_t terms = (heads + parts - 1) / parts, of_rows = TERMS / terms, enough = (most + of_rows - 1) / of_rows;   // TERMS / terms rows a wave
+        if (enough > blocks) blocks = enough > 1 << 22 ? 1 << 22 : enough;
+    }
+    g.blocks = (int)blocks;
+    g.q_parts = (int)(parts < q_heads ? parts : q_heads);
+    g.k_parts = (int)(parts < k_heads ? parts : k_heads);
     return g;
 }
 
@@ -353,7 +360,7 @@ template <typename T, bool BWD>
 hipError_t launch(const void *q, const void *k, const float *wq, const float *wk, const int32_t *pos, const float *freq, const void *gq, const void *gk, void *oq,
                   void *ok, int64_t ld_gq, int64_t ld_gk, int64_t ld_oq, int64_t ld_ok, const sn_headnorm_shape &s, float *part, hipStream_t st)
 {
-    const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads);
+    const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads, BWD);
     const HeadArgs h = {{{q, gq, oq, wq, s.ld_q, ld_gq, ld_oq, s.q_heads, g.q_parts}, {k, gk, ok, wk, s.ld_k, ld_gk, ld_ok, s.k_heads, g.k_parts}}, pos, freq, part,
                         (int)s.rows, s.head_dim, s.rot_dim, s.interleaved, s.eps};
     return by_size<T>(s.head_dim, s.rot_dim, s.q_heads > s.k_heads ? s.q_heads : s.k_heads, [&](auto E, auto NU, auto LPH) {
@@ -373,7 +380,7 @@ hipError_t launch_headnorm_fwd(const void *q, const void *k, const float *wq, co
 
 size_t headnorm_scratch_bytes(int64_t rows, int q_heads, int k_heads, int head_dim)
 {
-    const HeadGrid g = grid_of(rows, q_heads, k_heads);
+    const HeadGrid g = grid_of(rows, q_heads, k_heads, true);
     return align_up((size_t)g.blocks * (g.q_parts + g.k_parts) * head_dim * 4, 256);
 }
 
@@ -384,7 +391,7 @@ hipError_t launch_headnorm_bwd(const void *q, const void *k, const float *wq, co
         ? launch<bf16_t, true>(q, k, wq, wk, pos, freq, dyq, dyk, dq, dk, s.ld_yq, s.ld_yk, s.ld_dq, s.ld_dk, s, (float *)scratch, st)
         : launch<float, true>(q, k, wq, wk, pos, freq, dyq, dyk, dq, dk, s.ld_yq, s.ld_yk, s.ld_dq, s.ld_dk, s, (float *)scratch, st);
     if (e != hipSuccess || (!dwq && !dwk)) return e;
-    const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads);
+    const HeadGrid g = grid_of(s.rows, s.q_heads, s.k_heads, true);
     headnorm_sum_kernel<<<dim3((s.head_dim + 15) / 16, 2), 1024, 0, st>>>((const float *)scratch, dwq, dwk, s.head_dim, g.blocks * g.q_parts, g.blocks * g.k_parts);
     return hipGetLastError();
 }

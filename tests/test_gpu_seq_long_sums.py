@@ -53,3 +53,15 @@ def test_conv1d():
     a, b = float(np.float32(0.7)), float(np.float32(0.3))
     assert off(db, np.full(D, rows * b)) <= SUM
     assert off(dw, np.repeat([(rows - W + 1 + np.arange(W)) * a * b], D, 0)) <= SUM + 2.0 ** -24
+
+
+def test_headnorm():
+    rows, Dh = 1 << 25, 2
+    q = torch.tensor([[0.7, -1.3]], device="cuda").repeat(rows, 1)
+    dy, k = torch.full((rows, Dh), 0.3, device="cuda"), q[:, :Dh]
+    dq, dwq, dwk = torch.empty_like(q), torch.full((Dh,), SENTINEL, device="cuda"), torch.full((Dh,), SENTINEL, device="cuda")
+    sn.sn_headnorm_rot_bwd(q, k, None, None, None, None, dy, dy, dq, torch.empty_like(q), dwq, dwk, bytes_(sn.sn_headnorm_rot_scratch_bytes(rows, 1, 1, Dh)), Dh, 1e-6)
+    x = q[:1].double().cpu().numpy()
+    _, dw = oracle.headnorm_bwd(x, None, np.zeros(1), np.zeros(0), np.full((1, Dh), float(np.float32(0.3))), Dh, 1e-6, False)
+    for got in (dwq, dwk):      # a term: the squares' sum, the mean, eps, the root, two products
+        assert off(got, rows * dw) <= SUM + 8 * 2.0 ** -24
