@@ -119,6 +119,11 @@ struct LongSum {
     __device__ float total() const { return lost == lost ? s + lost : s; }
 };
 
+// a number as a type, for what chooses a kernel's template arguments
+template <int V> struct SeqInt { static constexpr int value = V; };
+
+inline int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
 // a slot index of a step call: row -> slot, or -1 for a row to skip
 __device__ inline int step_slot(const int32_t *slots, int row, int num_slots)
 {

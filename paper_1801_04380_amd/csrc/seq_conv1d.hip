@@ -350,18 +350,17 @@ __global__ void __launch_bounds__(THREADS) conv1d_step_kernel(const T *__restric
 }
 
 // f(type, width) with both as types
-template <int W> struct WidthIs { static constexpr int value = W; };
 template <typename F> hipError_t by_width(int width, F f)
 {
     switch (width) {
-    case 1: return f(WidthIs<1>());
-    case 2: return f(WidthIs<2>());
-    case 3: return f(WidthIs<3>());
-    case 4: return f(WidthIs<4>());
-    case 5: return f(WidthIs<5>());
-    case 6: return f(WidthIs<6>());
-    case 7: return f(WidthIs<7>());
-    default: return f(WidthIs<8>());
+    case 1: return f(SeqInt<1>());
+    case 2: return f(SeqInt<2>());
+    case 3: return f(SeqInt<3>());
+    case 4: return f(SeqInt<4>());
+    case 5: return f(SeqInt<5>());
+    case 6: return f(SeqInt<6>());
+    case 7: return f(SeqInt<7>());
+    default: return f(SeqInt<8>());
     }
 }
 
@@ -369,8 +368,6 @@ SeqRows rows_of(const sn_conv1d_shape &s, const int32_t *off)
 {
     return {off, s.seqs, (int)(s.rows / s.seqs), (int)s.rows};
 }
-
-int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Rows of a workgroup's run, a multiple of 16: about 512 workgroups over `blocks` channel blocks, two waves a SIMD, each with eight rows' loads on their
 // way; `least` rows at least, beside which the filters and the rows in front cost little: forward 16 (5003 x 1001 in fp32 12.8 us, with 32 14.8).
@@ -384,8 +381,8 @@ int run_of(int64_t rows, int blocks, int least)
 // The channels of a thread: MOST if there are as many (IN_WHOLE: and no rest), else 1.
 template <int MOST, bool IN_WHOLE, typename F> hipError_t by_vector(int channels, F f)
 {
-    if (channels >= MOST && !(IN_WHOLE && channels % MOST)) return f(WidthIs<MOST>());
-    return f(WidthIs<1>());
+    if (channels >= MOST && !(IN_WHOLE && channels % MOST)) return f(SeqInt<MOST>());
+    return f(SeqInt<1>());
 }
 
 template <typename T> hipError_t fwd(const void *x, const void *w, const float *bias, void *y, const sn_conv1d_shape &s, const int32_t *off, const void *state_in,
@@ -426,10 +423,13 @@ template <typename T> hipError_t bwd(const void *x, const void *w, const float *
         if (e != hipSuccess) return e;
         conv1d_sum_kernel<<<dim3(div_up(s.channels, 16), s.width + 1), THREADS, 0, st>>>((const float *)scratch, dw, dbias, s.channels, s.width, slices);
         e = hipGetLastError();
-        if (e != hipSuccess || !dstate_in || s.width == 1) return e;
-        conv1d_dstate_kernel<T, W.value><<<dim3(s.seqs, div_up(s.channels, THREADS)), THREADS, 0, st>>>(
-            (const T *)x, (const T *)w, bias, (const T *)dy, s.channels, s.silu, s.ld_x, s.ld_y, rows, (const T *)state_in, (const T *)dstate_out, (T *)dstate_in);
-        return hipGetLastError();
+        if (e != hipSuccess || !dstate_in) return e;
+        if constexpr (W.value > 1) {
+            conv1d_dstate_kernel<T, W.value><<<dim3(s.seqs, div_up(s.channels, THREADS)), THREADS, 0, st>>>(
+                (const T *)x, (const T *)w, bias, (const T *)dy, s.channels, s.silu, s.ld_x, s.ld_y, rows, (const T *)state_in, (const T *)dstate_out, (T *)dstate_in);
+            e = hipGetLastError();
+        }
+        return e;
     });
 }
 

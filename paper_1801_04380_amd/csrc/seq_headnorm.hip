@@ -329,8 +329,6 @@ HeadGrid grid_of(int64_t rows, int q_heads, int k_heads, bool sums)
     return g;
 }
 
-template <int V> struct Is { static constexpr int value = V; };
-
 // f(E, NU, LPH): the widest unit that the sizes allow, or a narrower one where a row's heads would leave half of a wave's lanes without work
 // (4099 rows, 8 and 8 heads of 16 in fp32, us forward and backward: units of 8 elements 7.4, 12.9, of 2 5.9, 7.6)
 template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, int heads, F f)
@@ -341,19 +339,24 @@ template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, 
     while (e > 1 && ((rot_dim / 2) % e || (head_dim - rot_dim) % e || heads * units_of(e) <= 32)) e /= 2;
     const int units = units_of(e);
     const auto pick = [&](auto E) {
-        if (units <= 1) return f(E, Is<1>(), Is<1>());
-        if (units <= 2) return f(E, Is<1>(), Is<2>());
-        if (units <= 4) return f(E, Is<1>(), Is<4>());
-        if (units <= 8) return f(E, Is<1>(), Is<8>());
-        if (units <= 16) return f(E, Is<1>(), Is<16>());
-        if (units <= 32) return f(E, Is<1>(), Is<32>());
-        if (units <= 64) return f(E, Is<1>(), Is<64>());
-        return f(E, Is<4>(), Is<64>());   // SN_HEADNORM_MAX_DIM / 2 units of one pair at most
+        if (units <= 1) return f(E, SeqInt<1>(), SeqInt<1>());
+        if (units <= 2) return f(E, SeqInt<1>(), SeqInt<2>());
+        if (units <= 4) return f(E, SeqInt<1>(), SeqInt<4>());
+        if (units <= 8) return f(E, SeqInt<1>(), SeqInt<8>());
+        if (units <= 16) return f(E, SeqInt<1>(), SeqInt<16>());
+        constexpr int largest = SN_HEADNORM_MAX_DIM / 2 / E.value;   // units that there can be
+        if constexpr (largest > 32)
+            if (units > 32) {
+                if constexpr (largest > 64)
+                    if (units > 64) return f(E, SeqInt<largest / 64>(), SeqInt<64>());
+                return f(E, SeqInt<1>(), SeqInt<64>());
+            }
+        return f(E, SeqInt<1>(), SeqInt<32>());
     };
-    if (e == 8) return pick(Is<most>());
-    if (e == 4) return pick(Is<4>());
-    if (e == 2) return pick(Is<2>());
-    return pick(Is<1>());
+    if (e == 8) return pick(SeqInt<most>());
+    if (e == 4) return pick(SeqInt<4>());
+    if (e == 2) return pick(SeqInt<2>());
+    return pick(SeqInt<1>());
 }
 
 template <typename T, bool BWD>

@@ -266,19 +266,18 @@ void scan_set_carry(ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, void
 hipError_t launch_scan_states(ScanArgs a, const sn_scan_shape &s, const ScanPlan &p, int wide, hipStream_t st);   // a.states from the inputs
 hipError_t launch_scan_carry(const ScanArgs &a, const ScanPlan &p, bool reverse, hipStream_t st);
 
-template <int V> struct ScanInt { static constexpr int value = V; };
 template <typename F> hipError_t by_lanes(int NL, F f)
 {
-    return NL == 2 ? f(ScanInt<2>()) : NL == 4 ? f(ScanInt<4>()) : NL == 8 ? f(ScanInt<8>()) : f(ScanInt<16>());
+    return NL == 2 ? f(SeqInt<2>()) : NL == 4 ? f(SeqInt<4>()) : NL == 8 ? f(SeqInt<8>()) : f(SeqInt<16>());
 }
 // f(lanes of a channel, width): with eight lanes and more a thread stages two channels at most, and twos are whole pieces
 template <typename F> hipError_t by_lanes_and_width(int NL, int wide, F f)
 {
     return by_lanes(NL, [&](auto L) {
-        if (wide == 2) return f(L, ScanInt<2>());
+        if (wide == 2) return f(L, SeqInt<2>());
         if constexpr (L.value < 8)
-            if (wide == 1) return f(L, ScanInt<1>());
-        return f(L, ScanInt<0>());
+            if (wide == 1) return f(L, SeqInt<1>());
+        return f(L, SeqInt<0>());
     });
 }
 

@@ -218,9 +218,9 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a, int reverse)
         }
     };
     int k = 0;   // the last chunk hands on to nothing: it has no values
-    for (; k + 16 < a.parts; k += 16) chunks(ScanInt<16>());
-    for (; k + 4 < a.parts; k += 4) chunks(ScanInt<4>());
-    for (; k + 1 < a.parts; ++k) chunks(ScanInt<1>());
+    for (; k + 16 < a.parts; k += 16) chunks(SeqInt<16>());
+    for (; k + 4 < a.parts; k += 4) chunks(SeqInt<4>());
+    for (; k + 1 < a.parts; ++k) chunks(SeqInt<1>());
     *to = v;
 }
 
@@ -301,8 +301,6 @@ template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape
         return hipGetLastError();
     });
 }
-
-int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 }  // namespace
 
