@@ -1,7 +1,8 @@
-// What the kernels of the token-sequence layers share: rows of packed sequences, element access at any alignment, sums over lanes.
+// What the kernels of the token-sequence layers share: element access at any alignment, exponentials, long sums.
 #pragma once
 #include "sn_internal.h"
 #include "sn_seq.h"
+#include "seq_walk.h"
 
 namespace sn {
 
@@ -33,50 +34,6 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Pack {
     __device__ float get(int i) const { return seq_ld<T>(&e[i]); }
     __device__ void set(int i, float v) { seq_st(&e[i], v); }
 };
-
-// The rows of packed sequences: off == nullptr: `seqs` sequences of `len` rows.  A row of no sequence has s outside 0 .. seqs - 1.  begin
-// and end stay within 0 .. rows whatever the offsets hold.
-struct SeqRows {
-    const int32_t *off;
-    int seqs, len, rows;
-};
-struct SeqAt {
-    int s, begin, end;  // the sequence of a row, its first row and the one behind its last
-    __device__ bool holds(int row, const SeqRows &r) const { return s >= 0 && s < r.seqs && begin <= row && row < end; }
-};
-__device__ inline SeqAt seq_clamped(const SeqRows &r, int s)
-{
-    SeqAt a;
-    a.s = s;
-    a.begin = s < 0 ? 0 : min(max(r.off[s], 0), r.rows);
-    a.end = s < r.seqs ? min(max(r.off[s + 1], 0), r.rows) : r.rows;
-    return a;
-}
-// The last sequence that begins at or before `row` (s = -1: none does; s = seqs: the row lies behind all of them).
-__device__ inline SeqAt seq_find(const SeqRows &r, int row)
-{
-    if (!r.off) {
-        SeqAt a;
-        a.s = row / r.len;
-        a.begin = a.s * r.len;
-        a.end = a.begin + r.len;
-        return a;
-    }
-    int lo = -1, hi = r.seqs + 1;  // off[lo] <= row < off[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (r.off[mid] <= row) lo = mid; else hi = mid;
-    }
-    return seq_clamped(r, lo);
-}
-// From the place of an earlier row on to that of `row`.
-__device__ inline void seq_forward(const SeqRows &r, SeqAt &a, int row)
-{
-    while (a.s < r.seqs && row >= a.end) {
-        if (r.off) a = seq_clamped(r, a.s + 1);
-        else { ++a.s; a.begin = a.end; a.end += r.len; }
-    }
-}
 
 // f(s) for the sequences without rows, by all lanes of a wave together: 64 offsets are looked at at a time.
 template <typename F> __device__ inline void each_empty(const SeqRows &r, F f)

@@ -42,53 +42,6 @@ struct ScanArgs {
     int gate;   // z is there; if not, z is u: loaded and left out
 };
 
-// The rows p0 .. p1 - 1 that one turn of a kernel's loop works on: those of one sequence in the tile of rows t0 .. t0 + ROWS - 1.  The tile's other
-// rows are staged as zeros: delta = 0 leaves the states, and the gradient on its way through them, as they are.
-struct Piece {
-    int t0, p0, p1, seq;
-    bool any, start, end;   // whether there is one; it begins, ends its sequence
-    __device__ bool holds(int row) const { return any && row >= p0 && row < p1; }
-};
-// The first piece at or behind row `from` of the chunk r0 .. r1 - 1.  `at`: the place of an earlier row.
-template <int ROWS> __device__ inline Piece piece_from(const SeqRows &r, SeqAt &at, int from, int r0, int r1)
-{
-    Piece p = {};
-    if (at.s < 0 && from < r1) at = seq_clamped(r, 0);
-    from = max(from, at.begin);
-    seq_forward(r, at, from);
-    from = max(from, at.begin);
-    if (at.s >= r.seqs || from >= r1 || from >= at.end) return p;
-    p.any = true;
-    p.seq = at.s;
-    p.p0 = from;
-    p.t0 = r0 + (from - r0) / ROWS * ROWS;
-    p.p1 = min(min(p.t0 + ROWS, at.end), r1);
-    p.start = from == at.begin;
-    p.end = p.p1 == at.end;
-    return p;
-}
-// The last piece in front of row `to`.  `at`: the place of a later row.
-template <int ROWS> __device__ inline Piece piece_before(const SeqRows &r, SeqAt &at, int to, int r0)
-{
-    Piece p = {};
-    if (at.s >= r.seqs && to > r0) at = seq_clamped(r, r.seqs - 1);
-    to = min(to, at.end);
-    while (at.s >= 0 && to > r0 && to <= at.begin) {
-        if (at.s == 0) at = SeqAt{-1, 0, 0};
-        else at = r.off ? seq_clamped(r, at.s - 1) : SeqAt{at.s - 1, at.begin - r.len, at.begin};
-        to = min(to, at.end);
-    }
-    if (at.s < 0 || to <= r0) return p;
-    p.any = true;
-    p.seq = at.s;
-    p.p1 = to;
-    p.t0 = r0 + (to - 1 - r0) / ROWS * ROWS;
-    p.p0 = max(p.t0, at.begin);
-    p.start = p.p0 == at.begin;
-    p.end = to == at.end;
-    return p;
-}
-
 // Lanes are numbered so that every bit of the number can be flipped by one cross-lane operand: bits 5 and 4 by the lane swaps, 3 by row_ror:8,
 // 1 and 0 by quad_perm.  For bit 2 there is only the mirror among eight lanes, which flips bits 1 and 0 of the hardware's
 // number as well; these two are therefore counted inverted where bit 2 is set.
