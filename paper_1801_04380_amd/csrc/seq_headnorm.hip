@@ -195,8 +195,8 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
             const bool turned = p.there && p.angle >= 0;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                co[u][i] = turned ? turn[wave][0][turned ? p.angle + i : 0] : 1.f;
-                si[u][i] = turned ? turn[wave][1][turned ? p.angle + i : 0] : 0.f;
+                co[u][i] = turn[wave][0][turned ? p.angle + i : 0];   // not used otherwise
+                si[u][i] = turn[wave][1][turned ? p.angle + i : 0];
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next row's are written
@@ -225,8 +225,9 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
                         const float na = v[u].a[i] * r * wa[u][i], nb = v[u].b[i] * r * wb[u][i];
-                        v[u].a[i] = na * co[u][i] - nb * si[u][i];
-                        v[u].b[i] = nb * co[u][i] + na * si[u][i];
+                        // what is not turned is left out by choice, not by a sine of 0: an infinity would come through as NaN
+                        v[u].a[i] = p.angle < 0 ? na : na * co[u][i] - nb * si[u][i];
+                        v[u].b[i] = p.angle < 0 ? nb : nb * co[u][i] + na * si[u][i];
                     }
                     v[u].store(o, p.pa, p.pb, p.nb, p.pairs);
                 }
@@ -234,9 +235,11 @@ __global__ void __launch_bounds__(THREADS) headnorm_kernel(HeadArgs h)
                 float dot = 0.f;
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
+                    const Place<E> p(u * LPH + l, h);
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        const float ga = d[u].a[i] * co[u][i] + d[u].b[i] * si[u][i], gb = d[u].b[i] * co[u][i] - d[u].a[i] * si[u][i];
+                        const float ga = p.angle < 0 ? d[u].a[i] : d[u].a[i] * co[u][i] + d[u].b[i] * si[u][i];
+                        const float gb = p.angle < 0 ? d[u].b[i] : d[u].b[i] * co[u][i] - d[u].a[i] * si[u][i];
                         v[u].a[i] *= r;
                         v[u].b[i] *= r;
                         dw[u][i][0] = fmaf(ga, v[u].a[i], dw[u][i][0]);
