@@ -65,3 +65,24 @@ def test_headnorm():
     _, dw = oracle.headnorm_bwd(x, None, np.zeros(1), np.zeros(0), np.full((1, Dh), float(np.float32(0.3))), Dh, 1e-6, False)
     for got in (dwq, dwk):      # a term: the squares' sum, the mean, eps, the root, two products
         assert off(got, rows * dw) <= SUM + 8 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("big", [float("inf"), 1e38])
+def test_sums_past_the_range_are_infinite(big):
+    """An infinite term, or terms whose sum is: not NaN, however the rows are cut."""
+    rows, D, N = 700, 8, 4
+    one, zero, vec = torch.ones(rows, D, device="cuda"), torch.zeros(rows, N, device="cuda"), torch.ones(D, device="cuda")
+    dy = torch.full_like(one, big)
+    dx, dw, db = torch.empty_like(one), torch.empty(D, 2, device="cuda"), torch.empty(D, device="cuda")
+    sn.sn_causal_conv1d_bwd(one, torch.zeros_like(dw), None, dy, dx, dw, db, bytes_(sn.sn_causal_conv1d_scratch_bytes(rows, D, 2)), silu=False)
+    # the first tap of the first row is on a zero in front of the sequence, and zero times an infinite dy is none
+    assert torch.isposinf(db).all() and torch.isposinf(dw[:, 1]).all() and (torch.isposinf(dw[:, 0]) | (big == float("inf"))).all()
+    shape = sn.scan_shape(rows, D, N, 1, 1, sn.SN_F32, False, False)
+    for n in sn.sn_scan_workspace_query(shape, sn.SN_SCAN_BWD):
+        A, dD = torch.zeros(D, N, device="cuda"), torch.empty(D, device="cuda")
+        sn.sn_scan_bwd(one, one, A, zero, zero, vec, None, None, dy, torch.empty_like(one), torch.empty_like(one), torch.empty_like(A), torch.empty_like(zero),
+                       torch.empty_like(zero), dD, None, None, bytes_(n + sn.sn_scan_states_bytes(shape)), softplus=False)
+        assert torch.isposinf(dD).all()
+    dwq, scratch = torch.empty(2, device="cuda"), bytes_(sn.sn_headnorm_rot_scratch_bytes(rows, 4, 0, 2))
+    sn.sn_headnorm_rot_bwd(one, None, None, None, None, None, dy, None, dx, None, dwq, None, scratch, 2)
+    assert torch.isposinf(dwq).all()
