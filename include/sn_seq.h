@@ -14,10 +14,10 @@
  *    front of the first) are neither read for any result nor written.  Offsets that descend, or leave 0 .. rows, give undefined results, but no access
  *    outside the tensors.
  *  - Sizes, SN_ERR_UNSUPPORTED beyond: rows 2^30 (of a step call 2^24 - 1), sequences 2^24 - 1, channels of the convolution 65535 * 256,
- *    channels of the scan 65535 blocks of 16 of one group.  Addresses are 64-bit.  rows = 0 is a valid call.
+ *    channels of the scan 65535 blocks of 16 of one group, heads of queries and keys together 2^20.  Addresses are 64-bit.  rows = 0 is a valid call.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
  *  - Arithmetic, states and sums are fp32; a result of `dtype` is rounded once.  Sums are in a fixed order: results are
- *    run-to-run identical.
+ *    run-to-run identical.  Those over rows are as exact as sums of about 256 terms, however many rows there are.
  */
 #ifndef SN_SEQ_H
 #define SN_SEQ_H
@@ -102,7 +102,7 @@ sn_status sn_headnorm_rot_bwd(const void *q, const void *k, const float *wq, con
  *   y = (sum_n C[t,g,n] * h[d,n] + D[d] * u) * (z ? z * sigmoid(z) : 1)
  * u, dt, z, y: rows x channels; B, C: rows x (groups * states); A: fp32 [channels][states]; D, dt_bias: fp32 [channels].  D, dt_bias
  * and z may be NULL.  h0, hT: fp32 [seqs][channels][states], the initial (NULL: zeros) and the final state; hT may be NULL, and must
- * not overlap h0.  Row strides of the scan stay below 2^24 elements (SN_ERR_UNSUPPORTED).
+ * not overlap h0.  Row strides of the scan are 2^24 elements at most (SN_ERR_UNSUPPORTED).
  * Workspace and speed: a call needs parallel work beyond channels x sequences only where these are few; then it cuts the
  * tokens into chunks whose states are joined through the workspace.  With less than preferred_bytes it cuts into fewer chunks, with
  * the least into none; the result differs by the rounding of the joins only. */
@@ -121,7 +121,8 @@ typedef struct {
 } sn_scan_shape;
 
 /* The strides of shape are not looked at here.  For SN_SCAN_BWD both sizes are those of a call that is given `states`; a call that is not
- * needs sn_scan_states_bytes(shape) more. */
+ * needs sn_scan_states_bytes(shape) more.  Sequences of equal length ask for what ragged ones ask for where they are many and short (to 16 tokens, and
+ * beyond as long as it saves more than an eighth); a few are walked side by side, with kept states and sums for whole tiles each. */
 sn_status sn_scan_workspace_query(const sn_scan_shape *shape, sn_scan_dir dir, size_t *min_bytes, size_t *preferred_bytes);
 
 /* What the backward pass needs of the forward pass: the state before every 16th token.  Kept (sn_scan_fwd's `states`) or left out and

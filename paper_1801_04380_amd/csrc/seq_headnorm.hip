@@ -333,7 +333,7 @@ HeadGrid grid_of(int64_t rows, int q_heads, int k_heads, bool sums)
 }
 
 // f(E, NU, LPH): the widest unit that the sizes allow, or a narrower one where a row's heads would leave half of a wave's lanes without work
-// (4099 rows, 8 and 8 heads of 16 in fp32, us forward and backward: units of 8 elements 7.4, 12.9, of 2 5.9, 7.6)
+// (4099 rows, 8 and 8 heads of 16 in fp32, us forward and backward: units of 8 elements 7.8, 12.9, of 2 6.5, 7.9)
 template <typename T, typename F> hipError_t by_size(int head_dim, int rot_dim, int heads, F f)
 {
     constexpr int most = 16 / (int)sizeof(T);

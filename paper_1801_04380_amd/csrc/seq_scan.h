@@ -4,7 +4,8 @@
 // one channel: NL neighbouring lanes (2, 4, 8 or 16 for up to 8, 16, 32, 64 states) hold a channel's, the wave 64 / NL channels.  Sums
 // over a channel's states then are four products in a lane and log2(NL) exchanges, shared by NL rows; sums over channels, which only the
 // gradients of B and C need, are exchanges among the lanes of like states, shared by 64 / NL values (scatter_sum).  The latter are the
-// more, so they have the bits of the lane number that exchange in two instructions a pair and not three.
+// more, so they have the bits of the lane number that exchange by lane swaps: two instructions a pair and not three, though as many issue slots, as
+// a swap takes two of them.
 // Rows are staged through LDS by all threads: delta, delta * u and the rest of what is per row and channel is computed once, not in every
 // lane of a channel.
 #pragma once

@@ -8,9 +8,10 @@
 // A tile's states are computed again from the one kept before it (eight rows of states and decays in registers at a time, four states a lane),
 // then the tile is walked backwards.  Three sums over a channel's states and two over a group's channels per row come on top of the
 // products: scatter_sum shares an exchange among as many values as it has lanes, 8 values a row and lane for dB and dC.  The sums of a
-// workgroup's channels go to the workspace and are joined by scan_join_kernel, in a fixed order.  Bound by the vector units: 104 instructions a row
-// and wave, of which 60 are the formulas' for four states, and busy in 84 % of the cycles at two waves a SIMD (registers; four waves spill
-// and are slower).  16384 x 2048 x 16: 492 us.  All 16 rows' states in registers at a time instead of eight, of which the second half's
+// workgroup's channels go to the workspace and are joined by scan_join_kernel, in a fixed order.  Bound by the vector units: 118 issue slots a row
+// and wave (105 instructions; exponentials and lane swaps take two slots), of which 56 are the formulas' for four states and 10 the second computation of
+// the first half's states, and busy in 83 % of the cycles at two waves a SIMD (registers; four waves spill
+// and are slower).  16384 x 2048 x 16: 502 us.  All 16 rows' states in registers at a time instead of eight, of which the second half's
 // are computed from the state between the halves: slower, at one wave a SIMD.
 // Cut into chunks like the forward pass where channels and sequences do not fill the chip: scan_bwd_local_kernel takes what a chunk hands to
 // the one before it, scan_carry_kernel joins.
