@@ -57,11 +57,26 @@ __device__ inline Pack<T, V> tap_input(const T *x, int64_t ld, const T *state, i
 
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict__ x, const T *__restrict__ w, const float *__restrict__ bias, T *__restrict__ y,
-                                                             int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, const T *__restrict__ state_in, T *__restrict__ state_out)
+                                                             int channels, int silu, int64_t ld_x, int64_t ld_y, SeqRows rows, int run, int runs,
+                                                             const T *__restrict__ state_in, T *__restrict__ state_out)
 {
     constexpr int R = 8;   // rows at a time: their loads are all on their way before the first is used
     const bool mine = (blockIdx.x * THREADS + threadIdx.x) * V < channels;
     const int c = mine ? min((int)(blockIdx.x * THREADS + threadIdx.x) * V, channels - V) : 0;
+    if ((int)blockIdx.y >= runs) {
+        each_empty(rows, blockIdx.y - runs, gridDim.y - runs, [&](int s) {
+            if (!mine) return;
+            const int64_t k = (int64_t)s * (W - 1) * channels + c;
+            Pack<T, V> v[W];   // all on their way before the first is stored
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+                if (state_in) v[j].load(state_in + k + (int64_t)j * channels);
+                else v[j].zero();
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) v[j].store(state_out + k + (int64_t)j * channels);
+        });
+        return;
+    }
     const int r0 = blockIdx.y * run, r1 = min(r0 + run, rows.rows);
     if (mine && r0 < r1) {
         Taps<T, V, W> taps;
@@ -118,16 +133,6 @@ __global__ void __launch_bounds__(THREADS) conv1d_fwd_kernel(const T *__restrict
             }
         }
     }
-    // the states of empty sequences pass through
-    if (state_out && W > 1 && blockIdx.y == 0 && (rows.off || rows.rows == 0))
-        each_empty(rows, [&](int s) {
-            if (!mine) return;
-            for (int j = 0; j < W - 1; ++j)
-                for (int i = 0; i < V; ++i) {
-                    const int64_t k = ((int64_t)s * (W - 1) + j) * channels + c + i;
-                    state_out[k] = state_in ? state_in[k] : (T)0;
-                }
-        });
 }
 
 // d y / d p
@@ -390,9 +395,12 @@ template <typename T> hipError_t fwd(const void *x, const void *w, const float *
 {
     return by_width(s.width, [&](auto W) {
         return by_vector<16 / sizeof(T), false>(s.channels, [&](auto V) {
-            const int blocks = div_up(s.channels, V.value * THREADS), run = run_of(s.rows, blocks, 16);
-            conv1d_fwd_kernel<T, V.value, W.value><<<dim3(blocks, s.rows ? div_up(s.rows, run) : 1), THREADS, 0, st>>>(
-                (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows_of(s, off), run, (const T *)state_in, (T *)state_out);
+            const SeqRows rows = rows_of(s, off);
+            const int blocks = div_up(s.channels, V.value * THREADS), run = run_of(s.rows, blocks, 16), runs = div_up(s.rows, run);
+            const int groups = runs + empty_groups(state_out && W.value > 1, rows);
+            if (!groups) return hipSuccess;
+            conv1d_fwd_kernel<T, V.value, W.value><<<dim3(blocks, groups), THREADS, 0, st>>>(
+                (const T *)x, (const T *)w, bias, (T *)y, s.channels, s.silu, s.ld_x, s.ld_y, rows, run, runs, (const T *)state_in, (T *)state_out);
             return hipGetLastError();
         });
     });

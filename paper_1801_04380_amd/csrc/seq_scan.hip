@@ -36,6 +36,14 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
     const int c0 = group * a.per_group + inside, nch = min(CB, a.per_group - inside);
     const int r0 = span * a.span_rows + part * a.chunk_rows, r1 = min(r0 + a.chunk_rows, (span + 1) * a.span_rows);
     const ScanLane<NL> lane(a, c0, nch);
+    if (OUT && chunk >= a.spans * a.parts) {
+        each_empty(a.rows, chunk - a.spans * a.parts, gridDim.x - a.spans * a.parts, [&](int s) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.h0) lane.load(a.h0, s, a, v);
+            lane.store(a.hT, s, a, v);
+        });
+        return;
+    }
     const int row = threadIdx.x / 16, co = threadIdx.x % 16 * VE, nco = nch - co, nl = scan_lane() % NL;
 
     float bias[VE], skip[VE];
@@ -171,12 +179,6 @@ __global__ void __launch_bounds__(THREADS) scan_fwd_kernel(ScanArgs a)
         if (lane.n0 == 0 && lane.there) a.sum_delta[(int64_t)chunk * a.channels + lane.channel] = sum_delta;
         if (blockIdx.y == 0 && threadIdx.x == 0) a.through[chunk] = !crossed;
     }
-    if (OUT && a.hT && chunk == 0 && (a.rows.off || a.rows.rows == 0))
-        each_empty(a.rows, [&](int s) {   // their states pass through
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (a.h0) lane.load(a.h0, s, a, v);
-            lane.store(a.hT, s, a, v);
-        });
 }
 
 // The state that each chunk starts from, in place of the one that it ends with from zero.  Reverse: the gradient of the state that
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(THREADS) scan_step_kernel(ScanArgs a, const fl
 template <int MODE> hipError_t launch_fwd(const ScanArgs &a, const sn_scan_shape &s, const ScanPlan &p, int wide, hipStream_t st)
 {
     return by_lanes_and_width(p.NL, wide, [&](auto NL, auto WIDE) {
-        const dim3 grid(p.chunks, p.blocks);
+        const dim3 grid(p.chunks + empty_groups(MODE == 0 && a.hT, a.rows), p.blocks);
         if (s.dtype == SN_BF16) scan_fwd_kernel<bf16_t, NL.value, WIDE.value, MODE><<<grid, THREADS, 0, st>>>(a);
         else scan_fwd_kernel<float, NL.value, WIDE.value, MODE><<<grid, THREADS, 0, st>>>(a);
         return hipGetLastError();

@@ -411,12 +411,6 @@ __global__ void __launch_bounds__(THREADS, 2) scan_bwd_kernel(ScanArgs a)
         }
     }
     add_sums(true);
-    if (a.dh0 && chunk == 0 && (a.rows.off || a.rows.rows == 0))
-        each_empty(a.rows, [&](int s) {   // the gradients of their states pass through
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (a.dhT) lane.load(a.dhT, s, a, v);
-            lane.store(a.dh0, s, a, v);
-        });
 }
 
 // dB and dC from the sums of the channel blocks: one thread per row, group, tensor and state, k counts them.
@@ -433,12 +427,32 @@ template <typename T> __device__ inline void join_bc(const ScanArgs &a, int grou
     seq_st((T *)to + group * a.N + n, sum);
 }
 
+// The gradients of empty sequences' states: of those that a group looks at, SLICE elements.
+constexpr int SLICE = 16 * THREADS;
+__device__ inline void pass_empty(const ScanArgs &a, int group, int count, int slice)
+{
+    const int64_t each = (int64_t)a.channels * a.N;
+    each_empty(a.rows, group, count, [&](int s) {
+#pragma unroll 4
+        for (int k = threadIdx.x; k < SLICE; k += THREADS) {
+            const int64_t i = (int64_t)slice * SLICE + k;
+            if (i < each) a.dh0[s * each + i] = a.dhT ? a.dhT[s * each + i] : 0.f;
+        }
+    });
+}
+
 // What is left to join, in one launch: the first `sums` workgroups take dA, dD and the bias's gradient from the sums of the chunks, 16 threads
-// along the chunks of each value, joined in a fixed order; the others dB and dC.
+// along the chunks of each value, joined in a fixed order; the next `bcs` dB and dC; the others, `empties` for each slice of a state, dh0 of empty sequences.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int groups, int chunks, unsigned sums, float *__restrict__ dA, float *__restrict__ dD, float *__restrict__ dbias)
+__global__ void __launch_bounds__(THREADS) scan_join_kernel(ScanArgs a, int groups, int chunks, unsigned sums, int64_t bcs, int empties, float *__restrict__ dA,
+                                                            float *__restrict__ dD, float *__restrict__ dbias)
 {
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (block >= sums + bcs) {
+        const int64_t k = block - sums - bcs;
+        if (empties) pass_empty(a, (int)(k % empties), empties, (int)(k / empties));
+        return;
+    }
     if (block >= sums) {
         join_bc<T>(a, groups, (block - sums) * THREADS + threadIdx.x);
         return;
@@ -530,11 +544,13 @@ hipError_t launch_scan_bwd(const void *u, const void *dt, const float *A, const 
         return bf16 ? bwd_in_chunks<bf16_t, NL.value, WIDE.value>(a, p, st) : bwd_in_chunks<float, NL.value, WIDE.value>(a, p, st);
     });
     if (e != hipSuccess) return e;
-    const int64_t sums = ((int64_t)s.channels * (s.states + 2) + 15) / 16, all = sums + (s.rows * s.groups * 8 * p.NL + THREADS - 1) / THREADS;
+    const int64_t sums = ((int64_t)s.channels * (s.states + 2) + 15) / 16, bcs = (s.rows * s.groups * 8 * p.NL + THREADS - 1) / THREADS;
+    const int empties = empty_groups(g.dh0, a.rows);
+    const int64_t all = sums + bcs + (int64_t)empties * div_up((int64_t)s.channels * s.states, SLICE);
     const int64_t most = 1 << 20;   // in x: a dimension of a grid has to stay below 2^32 threads
     const dim3 blocks((unsigned)(all < most ? all : most), (unsigned)((all + most - 1) / most));
-    if (bf16) scan_join_kernel<bf16_t><<<blocks, THREADS, 0, st>>>(a, s.groups, p.chunks, (unsigned)sums, g.dA, g.dD, g.ddt_bias);
-    else scan_join_kernel<float><<<blocks, THREADS, 0, st>>>(a, s.groups, p.chunks, (unsigned)sums, g.dA, g.dD, g.ddt_bias);
+    if (bf16) scan_join_kernel<bf16_t><<<blocks, THREADS, 0, st>>>(a, s.groups, p.chunks, (unsigned)sums, bcs, empties, g.dA, g.dD, g.ddt_bias);
+    else scan_join_kernel<float><<<blocks, THREADS, 0, st>>>(a, s.groups, p.chunks, (unsigned)sums, bcs, empties, g.dA, g.dD, g.ddt_bias);
     return hipGetLastError();
 }
 

@@ -1,7 +1,7 @@
 // Runs the host code of the token-sequence layers on a machine without a GPU, over sizes of all kinds, and prints which kernels it launches and
 // which there are: this program defines the runtime calls that the library makes, and the dynamic linker finds them here before the HIP
 // runtime's.  No kernel runs, no pointer is read.  A line each: `has <kernel>`, `launched <kernel>`, `bad <what>` (a grid beyond what the hardware
-// takes, a status that is not what the sizes ask for).
+// takes, a status that is not what the sizes ask for); at the end `grid <kernel> <workgroups>` of calls with many empty sequences.
 #include <cstdint>
 #include <cstdio>
 #include <map>
@@ -18,6 +18,7 @@ std::set<std::string> launched;
 Dim grid, block;
 size_t lds;
 void *stream;
+bool show;
 }  // namespace
 
 extern "C" {
@@ -33,6 +34,7 @@ int hipLaunchKernel(const void *f, Dim g, Dim b, void **, size_t, void *)
 {
     const std::string &name = names()[f];
     launched.insert(name);
+    if (show) std::printf("grid %s %llu\n", name.c_str(), (unsigned long long)g.x * g.y * g.z);
     const uint64_t threads = (uint64_t)g.x * b.x;
     if (!g.x || !g.y || !g.z || threads >= uint64_t(1) << 32 || g.y > 65535 || g.z > 65535) std::printf("bad grid %u %u %u of %s\n", g.x, g.y, g.z, name.c_str());
     return 0;
@@ -140,5 +142,14 @@ int main()
         want(sn_scan_bwd(at(0), at(1), fat(2), at(3), at(4), nullptr, nullptr, nullptr, at(8), at(13), at(14), fat(15), at(16), at(17), nullptr, nullptr, nullptr, &z, &off, fat(9),
                          fat(12), fat(22), fat(23), at(11), n, nullptr), "scan bwd of most rows");
     for (const auto &n : launched) std::printf("launched %s\n", n.c_str());
+    // a batch padded with empty sequences
+    show = true;
+    c = {800, 4096, 2048, 4, 1, SN_BF16, 2048, 2048, 2048};
+    want(sn_causal_conv1d_fwd(at(0), at(1), nullptr, at(3), &c, &off, at(4), at(5), nullptr), "conv fwd of empty sequences");
+    z = {800, 4096, 2048, 16, 1, SN_BF16, 1, 1, 2048, 2048, 16, 16, 2048, 2048, 2048, 2048, 16, 16, 2048};
+    want(sn_scan_workspace_query(&z, SN_SCAN_BWD, &least, &most), "scan query");
+    want(sn_scan_fwd(at(0), at(1), fat(2), at(3), at(4), nullptr, nullptr, nullptr, at(8), &z, &off, fat(9), fat(10), nullptr, nullptr, 0, nullptr), "scan fwd of empty sequences");
+    want(sn_scan_bwd(at(0), at(1), fat(2), at(3), at(4), nullptr, nullptr, nullptr, at(8), at(13), at(14), fat(15), at(16), at(17), nullptr, nullptr, nullptr, &z, &off, fat(9), fat(12),
+                     fat(22), fat(23), at(11), least, nullptr), "scan bwd of empty sequences");
     return 0;
 }
