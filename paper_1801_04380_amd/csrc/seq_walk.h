@@ -40,12 +40,26 @@ __device__ inline SeqAt seq_find(const SeqRows &r, int row)
     }
     return seq_clamped(r, lo);
 }
-// From the place of an earlier row on to that of `row`.
+// From the place of an earlier row on to that of `row`.  The next sequence mostly holds it; empty ones are passed by jumps that double as long as they do not go too
+// far, and else become half as long.
 __device__ inline void seq_forward(const SeqRows &r, SeqAt &a, int row)
 {
-    while (a.s < r.seqs && row >= a.end) {
-        if (r.off) a = seq_clamped(r, a.s + 1);
-        else { ++a.s; a.begin = a.end; a.end = a.s < r.seqs ? a.end + r.len : r.rows; }   // behind the last, the sum could pass 32 bits
+    for (int jump = 0; a.s < r.seqs && row >= a.end;) {
+        if (r.off) {
+            int s = a.s + 1;   // off[s] <= row
+            if (jump) {
+                const bool near = jump <= r.seqs - s && r.off[s + jump] <= row;
+                s = near ? s + jump : s;
+                jump = near ? 2 * jump : (jump + 1) / 2;
+            } else {
+                jump = 1;
+            }
+            a = seq_clamped(r, s);
+        } else {
+            ++a.s;
+            a.begin = a.end;
+            a.end = a.s < r.seqs ? a.end + r.len : r.rows;   // behind the last, the sum could pass 32 bits
+        }
     }
 }
 
@@ -80,12 +94,13 @@ template <int ROWS> __device__ inline Piece piece_before(const SeqRows &r, SeqAt
     Piece p = {};
     if (at.s >= r.seqs && to > r0) at = seq_clamped(r, r.seqs - 1);
     to = min(to, at.end);
-    while (at.s >= 0 && to > r0 && to <= at.begin) {
+    for (int turn = 0; turn < 2 && at.s >= 0 && to > r0 && to <= at.begin; ++turn) {   // the one in front, or, where that is empty, the last one that is not
         if (at.s == 0) at = SeqAt{-1, 0, 0};
+        else if (turn) at = seq_find(r, to - 1);
         else at = r.off ? seq_clamped(r, at.s - 1) : SeqAt{at.s - 1, at.begin - r.len, at.begin};
         to = min(to, at.end);
     }
-    if (at.s < 0 || to <= r0) return p;
+    if (at.s < 0 || at.s >= r.seqs || to <= r0 || to <= at.begin) return p;
     p.any = true;
     p.seq = at.s;
     p.p1 = to;

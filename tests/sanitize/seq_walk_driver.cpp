@@ -3,6 +3,7 @@
 // may give any result, but no row outside of the tensors, no sequence that there is not, and no loop without an end; valid ones give each row that a
 // sequence holds once, in its sequence.  Exit status 0 = all of it held and the sanitizers found nothing.
 #include <algorithm>
+#include <chrono>
 #include <climits>
 #include <cstdio>
 #include <cstdlib>
@@ -137,6 +138,28 @@ int main()
         Case c = {{nullptr, seqs, len, seqs * len}, true, {}};
         for (int t = 0; t < seqs * len; ++t) c.owner.push_back(t / len);
         walk(c);
+    }
+    // empty sequences, the most that a call may have, between two of eight rows: passed in a few steps (one after the other takes minutes here)
+    {
+        const int seqs = (1 << 24) - 1;
+        std::vector<int32_t> off(seqs + 1, 8);
+        off.front() = 0;
+        off.back() = 16;
+        const SeqRows r = {off.data(), seqs, 0, 16};
+        const auto start = std::chrono::steady_clock::now();
+        for (int i = 0; i < 1000; ++i) {
+            SeqAt at = seq_find(r, 0);
+            Piece p = piece_from<16>(r, at, 0, 0, 16);
+            CHECK(p.any && p.seq == 0 && p.p1 == 8);
+            p = piece_from<16>(r, at, 8, 0, 16);
+            CHECK(p.any && p.seq == seqs - 1 && p.p0 == 8 && p.p1 == 16 && p.start && p.end);
+            p = piece_before<16>(r, at, 8, 0);
+            CHECK(p.any && p.seq == 0 && p.p0 == 0 && p.p1 == 8 && p.start && p.end);
+            at = seq_find(r, 3);
+            seq_forward(r, at, 8);
+            CHECK(at.s == seqs - 1 && at.begin == 8 && at.end == 16);
+        }
+        CHECK(std::chrono::duration<double>(std::chrono::steady_clock::now() - start).count() < 5);
     }
     // the most rows that a call may have, in one sequence: nothing passes 32 bits at its end
     const int most = 1 << 30;
