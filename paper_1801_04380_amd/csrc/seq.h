@@ -36,8 +36,8 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Pack {
 };
 
 // The states of sequences without rows pass through: workgroups of their own, behind those that walk the rows, look at EMPTY_AT sequences at a time.  (One
-// workgroup for all of them took 16.3 ms over 800 rows and 4094 empty sequences of 2048 channels, four taps; with these and none walked one by one the call takes 0.03.)  They are there only
-// for calls that hand states on and may have such sequences.
+// workgroup for all of them took 16.3 ms over 800 rows and 4094 empty sequences of 2048 channels, four taps; with these, and none of
+// them walked one by one, the call takes 0.03.)  They are there only for calls that hand states on and may have such sequences.
 constexpr int EMPTY_AT = 16;
 inline int empty_groups(bool wanted, const SeqRows &r)
 {

@@ -5,7 +5,7 @@
 // Per row, channel and state: a product, an exponential (two issue slots: 16 of them take 1.89 ms where 16 fused products and sums take 0.94), and three
 // products and sums: six slots, against four tensors of rows x channels read and written.  With 16 states that is more time on the vector
 // units than in HBM: the kernel keeps them busy in all its cycles, with 40 slots a row and wave (35 instructions), of which 24 are the formula's for four
-// states.  16384 x 2048 x 16: 147 us, with the states kept; 32768 x 1024 x 16: 144 us, and 98 us for the chunks' own states before it.
+// states.  16384 x 2048 x 16: 147 us, with the states kept; 32768 x 1024 x 16: 143 us, and 98 us for the chunks' own states before it.
 // Where channels and sequences alone do not fill the chip the tokens are cut into chunks: a first pass takes every chunk's
 // final state from a zero one and its sum of delta (the product of its decays is exp(A * sum)), scan_carry_kernel joins them, and the
 // second pass starts each chunk from its state.

@@ -11,7 +11,7 @@
 // workgroup's channels go to the workspace and are joined by scan_join_kernel, in a fixed order.  Bound by the vector units: 118 issue slots a row
 // and wave (105 instructions; exponentials and lane swaps take two slots), of which 56 are the formulas' for four states and 10 the second computation of
 // the first half's states, and busy in 83 % of the cycles at two waves a SIMD (registers; four waves spill
-// and are slower).  16384 x 2048 x 16: 502 us.  All 16 rows' states in registers at a time instead of eight, of which the second half's
+// and are slower).  16384 x 2048 x 16: 501 us.  All 16 rows' states in registers at a time instead of eight, of which the second half's
 // are computed from the state between the halves: slower, at one wave a SIMD.
 // Cut into chunks like the forward pass where channels and sequences do not fill the chip: scan_bwd_local_kernel takes what a chunk hands to
 // the one before it, scan_carry_kernel joins.
